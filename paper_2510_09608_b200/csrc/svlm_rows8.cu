@@ -363,11 +363,15 @@ rows8_kernel(SvlmAttend8 a, int layer0, int n_layers, const uint16_t* Q, const i
     };
     load_keys(u0);
     load_values(u0);
-    // how far the middle of this thread block's units is from S: it has a copy of the queries of its own, the others turn theirs when they get there
+    // How far the middle of this thread block's units is from S: it has a copy of the queries of its own, the others turn theirs when they get there.
+    // All threads have to see one value (each warp puts its column into that copy, and all read it), so the block that the appended token joins
+    // has none: its word is the one that somebody may be writing meanwhile, another head's block of this launch or, with early, layer 0's.
     int apart0 = 0;
     if (!LAYER && total > 0) {
         int first;
-        if (tokens_of((int)((long long)total * (2 * split + 1) / (2 * splits)), first)) apart0 = max(0, ld_l2(vw.apart + first / SVLM_BLOCK8));
+        const unsigned tokens = tokens_of((int)((long long)total * (2 * split + 1) / (2 * splits)), first);
+        const bool joined = APPEND && new_slot >= 0 && (new_slot & ~(SVLM_BLOCK8 - 1)) == first;
+        if (tokens && !joined) apart0 = max(0, ld_l2(vw.apart + first / SVLM_BLOCK8));
     }
     // the appended token's rows come in with the queries, to the warp whose unit they join
     bool joins = false;
@@ -561,7 +565,8 @@ rows8_kernel(SvlmAttend8 a, int layer0, int n_layers, const uint16_t* Q, const i
             }
             result |= (unsigned)(ex & 255) << (8 * which);
         }
-        // (another head's thread blocks may have read it before or behind this: they come to the same)
+        // (other thread blocks' copies of this word may be of before or of behind this: the warp whose unit it is comes to the same here, nobody else
+        // uses it)
         apart = held && apart != 0 ? MIXED8 : 0;
         if (lane == 0) {
             vw.exps[at / SVLM_BLOCK8] = result;

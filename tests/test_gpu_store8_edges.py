@@ -1,0 +1,67 @@
+"""Caches that hold keys and values in 8 bits, where the kernels' paths meet: the statement, the comparison and its tolerances are
+test_gpu_store8.py's."""
+import numpy as np
+import pytest
+import torch
+
+from harness import dev_to_f64
+from paper_2510_09608_b200 import binding
+from store8 import bf16
+from test_gpu_store8 import Pair, close, to_dev
+
+pytestmark = pytest.mark.gpu
+
+
+def batched_step(ps, check=True):
+    """One generated token of every stream through all layers, in lock step."""
+    layers, hq, hk, d, n = ps[0].L, ps[0].hq, ps[0].hk, ps[0].d, len(ps)
+    pos = np.stack([p.place([0]) for p in ps]).reshape(n)
+    K, V = [p.normal(layers, 1, hk, d) for p in ps], [p.normal(layers, 1, hk, d) for p in ps]
+    Q = bf16(ps[0].rng.standard_normal((layers, n, hq, d)))
+    ty, qp = torch.zeros(n, dtype=torch.uint8, device="cuda"), torch.from_numpy(pos).cuda()
+    k, v, q = ([to_dev(np.stack([x[l, 0] for x in xs])) for l in range(layers)] for xs in (K, V, [Q[:, None, i] for i in range(n)]))
+    outs = [binding.decode_step_batched([p.cache for p in ps], l, k[l], v[l], ty if l == 0 else None, qp, q[l]) for l in range(layers)]
+    for i, p in enumerate(ps):
+        p.ref.append([0], pos[i:i + 1], K[i], V[i])
+        for l in range(layers):
+            close(dev_to_f64(outs[l])[i:i + 1], p.ref.attend(l, Q[l, i:i + 1], pos[i:i + 1]))
+        assert p.cache.status() == binding.OK
+
+
+@pytest.mark.parametrize("hq,hk,d", [(28, 4, 128), (4, 1, 64), (16, 2, 64)])
+@pytest.mark.parametrize("text", [40, 56, 120])
+def test_batched_steps_that_join_a_block_with_a_shift_of_its_own(hq, hk, d, text):
+    """An answer goes on in the last block of an earlier one, whose tokens all stand off by what has left behind them; that block is the middle
+    of a thread block's units (two of 16 tokens) and the one before it stands off as far.  Beside it a stream whose tokens are all off
+    differently and one that has lost nothing, in the same launches."""
+    ps = [Pair(500 + i, layers=3, hq=hq, hk=hk, d=d, sink=0, vw=16, tw=300) for i in range(3)]
+    for rnd in range(2):
+        ps[0].append([0] * text if rnd == 0 else [0] * 32)
+        ps[0].append([1] * 64)
+        ps[1].append([0, 1] * 28)
+        ps[2].append([0] * 20 + [1] * 10)
+        binding.evict_batched([ps[0].cache, ps[1].cache, ps[2].cache])
+        for p in ps:
+            p.ref.evict()
+        for _ in range(4):
+            batched_step(ps)
+        for p in ps:
+            p.check()
+
+
+@pytest.mark.parametrize("text", [40, 56])
+def test_all_layers_steps_that_join_a_block_with_a_shift_of_its_own(text):
+    """The same in one launch for all layers of one stream."""
+    p = Pair(520 + text, layers=3, hq=8, hk=2, d=128, sink=0, vw=16, tw=300)
+    p.append([0] * text)
+    p.append([1] * 64)
+    p.evict()
+    for _ in range(3):
+        pos = p.place([0])
+        K, V, Q = p.normal(3, 1, 2, 128), p.normal(3, 1, 2, 128), bf16(p.rng.standard_normal((3, 1, 8, 128)))
+        zero = torch.zeros(1, dtype=torch.uint8, device="cuda")
+        out = dev_to_f64(p.cache.decode_step(-1, to_dev(K), to_dev(V), zero, torch.from_numpy(pos).cuda(), to_dev(Q)))
+        p.ref.append([0], pos, K, V)
+        for l in range(3):
+            close(out[l], p.ref.attend(l, Q[l], pos))
+    p.check()

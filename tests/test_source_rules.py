@@ -75,3 +75,17 @@ def test_a_decode_step_that_appends_lets_nobody_start_beside_it():
     src = _source("svlm_decode.cu")
     starts = [line.strip() for line in src.splitlines() if "pdl_launch_dependents" in line]
     assert len(starts) == 2 and all(line.startswith("if (!Append::on)") for line in starts), starts
+
+
+def test_what_an_appending_launch_may_change_is_not_read_by_every_thread_for_itself():
+    """An 8-bit cache's `apart` of the block that a generated token joins is written while other thread blocks, or the next layer's launch,
+    begin.  Outside a warp's asynchronous copy (one word for all its lanes) it is read for the block's middle unit, which all
+    threads must take for one value: not where that unit is the one the token joins."""
+    src = _source("svlm_rows8.cu")
+    direct = [m.start() for m in re.finditer(r"ld_l2\(vw\.apart\b", src)]
+    assert len(direct) == 1
+    statement = src[src.rindex(";", 0, direct[0]):src.index(";", direct[0])]
+    assert "!joined" in statement
+    assert re.search(r"const bool joined = APPEND && new_slot >= 0 && \(new_slot & ~\(SVLM_BLOCK8 - 1\)\) == first;", src)
+    # what else touches it: the copy of a warp's units, the joining warp's store
+    assert len(re.findall(r"vw\.apart\b", src)) == 3
