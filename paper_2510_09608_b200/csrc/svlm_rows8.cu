@@ -129,6 +129,9 @@ struct R8 {
     static constexpr int COPIES = 2 + R8_WARPS * R8_SLOTS;          // of the queries: for s = S, for the middle of the block's units, and each warp's latest ones
     static constexpr size_t smem(int n_pages) { return work_bytes + COPIES * frag_bytes + (sizeof(Small) + 15) / 16 * 16 + (size_t)n_pages * 4; }
 };
+// What a product of a query in its units and a key in its own is to be multiplied by.  The two units first: either may be large and the other
+// small.  Above 0, however small (a query of zeros, keys next to nothing): what hides a token is a score of -inf, which stays one.  Finite.
+__device__ __forceinline__ float score_unit(float q_unit, float k_unit) { return fminf(fmaxf(q_unit * k_unit, 1.2e-38f), 3.0e38f); }
 // Where a row's 16-byte chunk lies in a slot: so that eight lanes' 16 bytes fall into different banks.
 template <int D>
 __device__ __forceinline__ int chunk_at(int row, int chunk) { return row * D + ((chunk ^ (D == 128 ? row & 7 : (row >> 1) & 3)) << 4); }
@@ -468,8 +471,8 @@ rows8_kernel(SvlmAttend8 a, int layer0, int n_layers, const uint16_t* Q, const i
             hi[e] = live ? __uint_as_float((unsigned)q_hi[c][e] << 16) : 0.f;
             most = max(most, max(__float_as_uint(lo[e]) & 0x7fffffffu, __float_as_uint(hi[e]) & 0x7fffffffu));
         }
-        // units: the row's largest magnitude is in [1, 2) of them
-        const int ex = max(-126, min(126, (int)(__reduce_max_sync(0xffffffffu, most) >> 23) - 127));
+        // units: the row's largest magnitude is in [1, 2) of them (a smaller row's, zeros among them, of 2^-120: q_unit is a normal number)
+        const int ex = max(-120, min(126, (int)(__reduce_max_sync(0xffffffffu, most) >> 23) - 127));
         const float f = pow2i(-ex);
         float put_lo[PPL], put_hi[PPL];
 #pragma unroll
@@ -668,6 +671,11 @@ rows8_kernel(SvlmAttend8 a, int layer0, int n_layers, const uint16_t* Q, const i
 #pragma unroll
         for (int i = 0; i < R8_SLOTS; ++i) {
             const float ku = pow2i(exponent_of(exps[i], 0));
+            float f[R8_TILES][2];
+#pragma unroll
+            for (int n = 0; n < R8_TILES; ++n)
+#pragma unroll
+                for (int c = 0; c < 2; ++c) f[n][c] = score_unit(sh.q_unit[n * 8 + 2 * t + c], ku);
             int rel[2] = {0, 0};
             bool causal = false;
             if (!ONE) {
@@ -684,7 +692,7 @@ rows8_kernel(SvlmAttend8 a, int layer0, int n_layers, const uint16_t* Q, const i
                 for (int e = 0; e < 4; ++e) {
                     const int col = n * 8 + 2 * t + (e & 1);
                     const bool in = ((valid[i] >> (g + 8 * (e >> 1))) & 1) && (!causal || rel[e >> 1] <= sh.q_tok[col]);
-                    s[i][n][e] = in ? s[i][n][e] * sh.q_unit[col] * ku : -INFINITY;
+                    s[i][n][e] = in ? s[i][n][e] * f[n][e & 1] : -INFINITY;
                     mx[i][n][e & 1] = fmaxf(mx[i][n][e & 1], s[i][n][e]);
                     if (!ONE && causal) {          // lane 4 g + t knows of token g + 8 (e / 2) and column 2 t + e % 2
                         const unsigned they = __ballot_sync(0xffffffffu, in) >> t;
@@ -854,10 +862,10 @@ rows8_kernel(SvlmAttend8 a, int layer0, int n_layers, const uint16_t* Q, const i
                             if (!((valid[i] >> (g + 8 * (e >> 1))) & 1)) s[i][0][e] = -INFINITY;
                 }
                 float mx[2] = {-INFINITY, -INFINITY};
-                const float big = 3.0e38f, qu[2] = {sh.q_unit[2 * t], sh.q_unit[2 * t + 1]};
+                const float qu[2] = {sh.q_unit[2 * t], sh.q_unit[2 * t + 1]};
 #pragma unroll
                 for (int i = 0; i < R8_SLOTS; ++i) {
-                    const float ku = pow2i(exponent_of(exps[i], 0)), f[2] = {fminf(qu[0] * ku, big), fminf(qu[1] * ku, big)};
+                    const float ku = pow2i(exponent_of(exps[i], 0)), f[2] = {score_unit(qu[0], ku), score_unit(qu[1], ku)};
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         s[i][0][e] *= f[e & 1];

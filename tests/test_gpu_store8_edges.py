@@ -65,3 +65,31 @@ def test_all_layers_steps_that_join_a_block_with_a_shift_of_its_own(text):
         for l in range(3):
             close(out[l], p.ref.attend(l, Q[l], pos))
     p.check()
+
+
+def tiny(p, n, hk, d, up):
+    return bf16(p.normal(1, n, hk, d) * 2.0 ** up)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("n", [1, 5, 21, 40, 200])
+def test_a_query_of_zeros_gives_the_mean(d, n):
+    """One head's query is zero, another's next to nothing: equal weights for all stored tokens, whatever units the keys are in (blocks that
+    are partly filled or missing in a pair; zero keys and tiny ones); the heads beside them are as they were."""
+    for up in (0, -40, -110, None):
+        p = Pair(600 + n, hq=8, hk=2, d=d, sink=2, vw=150, tw=100, capacity=512)
+        K = None if up == 0 else np.zeros((1, n, 2, d)) if up is None else tiny(p, n, 2, d, up)
+        p.append(p.rng.integers(0, 2, n), K=K)
+        for n_q in (1, min(n, 3)):
+            Q, pos = bf16(p.rng.standard_normal((n_q, 8, d))), p.pos[-n_q:]
+            Q[:, 1], Q[:, 6] = 0, bf16(Q[:, 6] * 2.0 ** -122)
+            got = dev_to_f64(p.cache.attend(0, to_dev(Q), torch.from_numpy(np.ascontiguousarray(pos)).cuda()))
+            close(got, p.ref.attend(0, Q, pos))
+        p.evict()
+        pos, V = p.place([0]), p.normal(1, 1, 2, d)
+        K = p.normal(1, 1, 2, d) if up == 0 else np.zeros((1, 1, 2, d)) if up is None else tiny(p, 1, 2, d, up)
+        Q = np.zeros((1, 8, d))
+        Q[0, 3] = bf16(p.rng.standard_normal(d))
+        out = p.cache.decode_step(0, to_dev(K[0]), to_dev(V[0]), torch.zeros(1, dtype=torch.uint8, device="cuda"), torch.from_numpy(pos).cuda(), to_dev(Q))
+        p.ref.append([0], pos, K, V)
+        close(dev_to_f64(out), p.ref.attend(0, Q, pos))
