@@ -1192,7 +1192,8 @@ prefill_kernel(const __grid_constant__ SvlmAttendBatch b, const __grid_constant_
             pages.begin(sh);
             // the power of two of the head's keys stands behind the cache's descriptors
             if (HALF) unit += ld_l2(reinterpret_cast<const int*>(reinterpret_cast<const unsigned char*>(w.vw->tmaps) + 512) + gr.rows.hk);
-            const float c_row = pf_scale<D> * __int_as_float((127 + max(-126, min(120, unit))) << 23);
+            // (Not below 2^-120, so that c_row is a normal number: a row of zeros has the least unit there is, and a hidden score, -inf, times 0 would be NaN.)
+            const float c_row = pf_scale<D> * __int_as_float((127 + max(-120, min(120, unit))) << 23);
             for (int j = 0; j < n_proc; ++j) {
                 const unsigned pi = pages.next(w, r_lo);
                 const bool masked = (pi >> 28) & 1;

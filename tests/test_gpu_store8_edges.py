@@ -93,3 +93,20 @@ def test_a_query_of_zeros_gives_the_mean(d, n):
         out = p.cache.decode_step(0, to_dev(K[0]), to_dev(V[0]), torch.zeros(1, dtype=torch.uint8, device="cuda"), torch.from_numpy(pos).cuda(), to_dev(Q))
         p.ref.append([0], pos, K, V)
         close(dev_to_f64(out), p.ref.attend(0, Q, pos))
+
+
+@pytest.mark.parametrize("hq,hk,d,n", [(8, 2, 128, 150), (28, 4, 128, 140), (8, 2, 64, 200), (8, 1, 64, 300)])
+def test_query_rows_of_zeros_in_a_long_chunk(hq, hk, d, n):
+    """A chunk that goes over a widened layer, some of whose rows are zero (padding) or next to nothing: the mean of what they see, and the other
+    rows as ever; over ordinary keys, tiny ones and zeros."""
+    for up in (0, -60, None):
+        p = Pair(660 + n, hq=hq, hk=hk, d=d, sink=2, vw=300, tw=200, capacity=900)
+        p.append(p.rng.integers(0, 2, 170))
+        p.evict()
+        K = None if up == 0 else np.zeros((1, n, hk, d)) if up is None else tiny(p, n, hk, d, up)
+        p.append(p.rng.integers(0, 2, n), K=K)
+        Q, pos = bf16(p.rng.standard_normal((n, hq, d))), p.pos
+        Q[3:20], Q[40, 1], Q[n - 1, hq - 1], Q[70] = 0, 0, 0, bf16(Q[70] * 2.0 ** -123)
+        got = dev_to_f64(p.cache.attend(0, to_dev(Q), torch.from_numpy(np.ascontiguousarray(pos)).cuda()))
+        assert p.cache.status() == binding.OK
+        close(got, p.ref.attend(0, Q, pos))
