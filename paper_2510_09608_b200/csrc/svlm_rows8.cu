@@ -19,8 +19,9 @@
 // 2t, 2t + 1, 2t + 8, 2t + 9, paired by byte permutes.  e4m3 is exact in f16, so the MMAs are m16n8k16 in f16 with fp32 sums.
 // Roundings on the way: the turned query, in units of a power of two of its row, to f16 (2^-12), and a turned key; the weights to f16,
 // relative to the largest weight times unit that the row has met: w = 2^(s + ve - R), R the running maximum of s + ve (s in powers of
-// two), so that values far apart in different blocks neither overflow nor vanish.  The sum of the weights has its own running maximum, in
-// fp32.  A split's partial result goes to those that merge it as bf16, its maximum and sum as fp32.
+// two), so that values far apart in different blocks neither overflow nor vanish.  The sum of the weights has its own running maximum m, in
+// fp32, and R is kept as R - m: the sum of a score of thousands and a unit would be rounded, and with it the size of the output (scores of 2^32
+// gave outputs 2^7 and 2^14 times too large).  A split's partial result goes to those that merge it as bf16, its maximum and sum as fp32.
 // A thread block has 8 columns, query rows of a KV head; the others are other blocks', which read the units again out of L2.
 // Instances: one query token of up to 8 heads (ONE), with and without its append, for one layer of one cache (LAYER) and for several; anything else.
 //
@@ -121,7 +122,7 @@ struct R8 {
     struct Small {
         float q_unit[COLS];                        // power of two of a column's query, times log2(e) / sqrt(D)
         int q_tok[COLS];                           // its token of the chunk
-        float m[R8_WARPS][COLS], r[R8_WARPS][COLS], l[R8_WARPS][COLS];      // maxima of s and of s + ve; sums
+        float m[R8_WARPS][COLS], r[R8_WARPS][COLS], l[R8_WARPS][COLS];      // maxima of s; of s + ve, less those; sums
         float2 cs[HALF];                           // the appended token's rotation
         int last, tag;
         unsigned wait_limit;
@@ -505,7 +506,7 @@ rows8_kernel(SvlmAttend8 a, int layer0, int n_layers, const uint16_t* Q, const i
     __syncthreads();
 
     float o[R8_TILES][C::KS][4];
-    float m[R8_TILES][2], r[R8_TILES][2], l[R8_TILES][2];            // of columns 2t, 2t + 1: maximum of s, of s + ve; this lane's share of the sum
+    float m[R8_TILES][2], r[R8_TILES][2], l[R8_TILES][2];            // of columns 2t, 2t + 1: maximum of s; of s + ve, less that; this lane's share of the sum
 #pragma unroll
     for (int n = 0; n < R8_TILES; ++n) {
 #pragma unroll
@@ -722,12 +723,14 @@ rows8_kernel(SvlmAttend8 a, int layer0, int n_layers, const uint16_t* Q, const i
             float mu[2], ru[2];
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
-                const float mn = fmaxf(m[n][c], fmaxf(mx[0][n][c], mx[1][n][c])), rn = fmaxf(r[n][c], fmaxf(mx[0][n][c] + ve[0], mx[1][n][c] + ve[1]));
+                const float mn = fmaxf(m[n][c], fmaxf(mx[0][n][c], mx[1][n][c]));
                 mu[c] = mn == -INFINITY ? 0.f : mn;
+                const float down = m[n][c] - mu[c], was = r[n][c] + down;          // -inf where there was nothing
+                const float rn = fmaxf(was, fmaxf((mx[0][n][c] - mu[c]) + ve[0], (mx[1][n][c] - mu[c]) + ve[1]));
                 ru[c] = rn == -INFINITY ? 0.f : rn;
-                l[n][c] *= exp2f(m[n][c] - mu[c]);                  // m = -inf gives 0
-                corr[n][c] = exp2f(r[n][c] - ru[c]);
-                grows |= rn != r[n][c];
+                l[n][c] *= exp2f(down);
+                corr[n][c] = exp2f(was - ru[c]);
+                grows |= rn != was;
                 m[n][c] = mn;
                 r[n][c] = rn;
             }
@@ -736,8 +739,9 @@ rows8_kernel(SvlmAttend8 a, int layer0, int n_layers, const uint16_t* Q, const i
                 float w[4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    l[n][e & 1] += exp2f(s[i][n][e] - mu[e & 1]);
-                    w[e] = exp2f(s[i][n][e] + (ve[i] - ru[e & 1]));
+                    const float x = s[i][n][e] - mu[e & 1];
+                    l[n][e & 1] += exp2f(x);
+                    w[e] = exp2f(x + (ve[i] - ru[e & 1]));
                 }
                 p[i][n].x = movmatrix_trans(pack_half2(w[0], w[1]));
                 p[i][n].y = movmatrix_trans(pack_half2(w[2], w[3]));
@@ -847,7 +851,7 @@ rows8_kernel(SvlmAttend8 a, int layer0, int n_layers, const uint16_t* Q, const i
             float s[R8_SLOTS][R8_TILES][4] = {};
             scores(u0, s);
             // Nothing has gone before, so there is nothing to rescale, and the two units' weights share a reference where their values' units are not
-            // far apart: w = 2^(s - m) 2^(ve - vmax + 8), R = m + vmax - 8.  (What is behind the wait is paid by the instruction: code that runs once in a
+            // far apart: w = 2^(s - m) 2^(ve - vmax + 8), R - m = vmax - 8.  (What is behind the wait is paid by the instruction: code that runs once in a
             // launch runs at the pace of its fetching, 4 to 8 cycles each.)
             const int vmax = max(exponent_of(exps[0], 1), valid[1] ? exponent_of(exps[1], 1) : -127);
             const int below[R8_SLOTS] = {vmax - exponent_of(exps[0], 1), valid[1] ? vmax - exponent_of(exps[1], 1) : 0};
@@ -897,7 +901,7 @@ rows8_kernel(SvlmAttend8 a, int layer0, int n_layers, const uint16_t* Q, const i
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
                     m[0][c] = mx[c];
-                    r[0][c] = mx[c] + (float)(vmax - 8);
+                    r[0][c] = (float)(vmax - 8);
                 }
                 outputs(u0, p);
             }
@@ -955,7 +959,7 @@ rows8_kernel(SvlmAttend8 a, int layer0, int n_layers, const uint16_t* Q, const i
         for (int w = 0; w < R8_WARPS; ++w) {
             const float mw = sh.m[w][col];
             const bool none = mw == -INFINITY;                      // no score, or none that is a number
-            const float f = none ? 0.f : exp2f(sh.r[w][col] - M);   // back from s + ve to s
+            const float f = none ? 0.f : exp2f((mw - M) + sh.r[w][col]);         // back from s + ve to s
             const float4 x = *reinterpret_cast<const float4*>(result_of(w) + col * ROW + d0);
             acc[0] += x.x * f; acc[1] += x.y * f; acc[2] += x.z * f; acc[3] += x.w * f;
             if (d0 == 0 || splits == 1) L += sh.l[w][col] * (none ? 1.f : exp2f(mw - M));

@@ -110,3 +110,37 @@ def test_query_rows_of_zeros_in_a_long_chunk(hq, hk, d, n):
         got = dev_to_f64(p.cache.attend(0, to_dev(Q), torch.from_numpy(np.ascontiguousarray(pos)).cuda()))
         assert p.cache.status() == binding.OK
         close(got, p.ref.attend(0, Q, pos))
+
+
+@pytest.mark.parametrize("n_q", [1, 3])
+def test_large_queries_over_small_keys(n_q):
+    """Queries of 2^126 over keys of 400 * 2^-100: the product in the query's unit alone is no float, the scores (+-400 * 2^26 / sqrt(128)) are, and
+    one token has all the weight.  (That direction turns with the position by less than 0.02.)"""
+    p = Pair(640 + n_q, hq=8, hk=2, d=128, sink=2, vw=150, tw=100, capacity=512)
+    K = np.zeros((1, 90, 2, 128))
+    K[..., 63] = -400 * 2.0 ** -100
+    K[0, 7, :, 63] *= -1
+    p.append(p.rng.integers(0, 2, 90), K=bf16(K))
+    Q, pos = np.zeros((n_q, 8, 128)), p.pos[-n_q:]
+    Q[..., 63] = 2.0 ** 126
+    got = dev_to_f64(p.cache.attend(0, to_dev(Q), torch.from_numpy(np.ascontiguousarray(pos)).cuda()))
+    want = p.ref.attend(0, Q, pos)
+    close(got, want)
+    assert np.abs(want - p.ref.V[(7, 0)][np.arange(8) // 4]).max() == 0
+
+
+@pytest.mark.parametrize("up", [8, 12, 16, 20])
+@pytest.mark.parametrize("n", [20, 300])
+def test_large_scores_leave_the_size_of_the_output_alone(n, up):
+    """All values are 1.75, and so is every output, whatever the weights: scores of about 2^up; one token, appended or not, and a few rows."""
+    p = Pair(650 + up, hq=8, hk=2, d=64, sink=2, vw=400, tw=200, capacity=900)
+    V = np.ones((1, n, 2, 64)) * 1.75
+    p.append(p.rng.integers(0, 2, n), V=V, K=bf16(p.normal(1, n, 2, 64) * 2.0 ** (up - 3)))
+    for n_q in (1, 4):
+        Q, pos = bf16(p.rng.standard_normal((n_q, 8, 64))), p.pos[-n_q:]
+        got = dev_to_f64(p.cache.attend(0, to_dev(Q), torch.from_numpy(np.ascontiguousarray(pos)).cuda()))
+        close(got, np.full(got.shape, 1.75))
+    pos, K, Q = p.place([0]), bf16(p.normal(1, 1, 2, 64) * 2.0 ** (up - 3)), bf16(p.rng.standard_normal((1, 8, 64)))
+    V = np.ones((1, 1, 2, 64)) * 1.75
+    out = p.cache.decode_step(0, to_dev(K[0]), to_dev(V[0]), torch.zeros(1, dtype=torch.uint8, device="cuda"), torch.from_numpy(pos).cuda(), to_dev(Q))
+    close(dev_to_f64(out), np.full((1, 8, 64), 1.75))
