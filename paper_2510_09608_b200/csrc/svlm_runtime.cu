@@ -400,7 +400,7 @@ int attend_common(svlm_cache* const* caches, int n_caches, int layer, const void
         }
         return SVLM_OK;
     }
-    if (split_kv && !decode_aligned(Q, Knew, Vnew, out, q_pos)) return SVLM_ERR_ARG;
+    if ((split_kv || few8) && !decode_aligned(Q, Knew, Vnew, out, q_pos)) return SVLM_ERR_ARG;      // (8-bit caches' kernel writes words whatever the shape)
     if (chunk && !(aligned(16, Q, out) && aligned(4, q_pos))) return SVLM_ERR_ARG;      // (the general kernel reads and writes element by element)
     SvlmAttendBatch b;
     b.n_caches = n_caches;
