@@ -401,7 +401,7 @@ int attend_common(svlm_cache* const* caches, int n_caches, int layer, const void
         return SVLM_OK;
     }
     if ((split_kv || few8) && !decode_aligned(Q, Knew, Vnew, out, q_pos)) return SVLM_ERR_ARG;      // (8-bit caches' kernel writes words whatever the shape)
-    if (chunk && !(aligned(16, Q, out) && aligned(4, q_pos))) return SVLM_ERR_ARG;      // (the general kernel reads and writes element by element)
+    if (!aligned(chunk ? 16 : 2, Q, out) || !aligned(4, q_pos)) return SVLM_ERR_ARG;      // (the general kernel reads and writes element by element)
     SvlmAttendBatch b;
     b.n_caches = n_caches;
     fill_batch_geometry(c0, b);
@@ -677,7 +677,7 @@ int svlm_cache_append(svlm_cache* c, int layer, const void* K, const void* V, co
     DeviceGuard guard(c->device);
     c->last_decode_layer = -1;
     if (layer <= 0) {
-        if (!token_type || !pos) return SVLM_ERR_ARG;
+        if (!token_type || !pos || !aligned(4, pos)) return SVLM_ERR_ARG;
         if (n > c->dev.capacity) return SVLM_ERR_CAPACITY;
         c->configured_locked = true;
         if (!c->bits8 && svlm_append_in_one(c->dev, layer, n)) {
@@ -715,7 +715,7 @@ int svlm_qkv_append(svlm_cache* c, int layer, const void* X, const void* W, int 
         return SVLM_ERR_CUDA;
     c->last_decode_layer = -1;
     if (layer == 0) {
-        if (!token_type || !pos) return SVLM_ERR_ARG;
+        if (!token_type || !pos || !aligned(4, pos)) return SVLM_ERR_ARG;
         if (n > c->dev.capacity) return SVLM_ERR_CAPACITY;
         c->configured_locked = true;
         SVLM_CUDA(svlm_launch_append_meta(c->dev, token_type, pos, n, c->stream));

@@ -31,3 +31,25 @@ for call in (lambda **kw: attend(wide, 1, hq=4, **kw), lambda **kw: attend(wide,
     assert call(Q=P + 2, out=P + 4) == OK
     assert any("rows8" in k for k in ran())
 """)
+
+
+def test_positions_are_words(host):  # noqa: F811
+    """Positions that do not begin at a word, of an append, of a projection that appends and of the general attention kernel: refused before anything runs."""
+    host(NEW8 + """
+for c in (new(), new8()):
+    for layer in (-1, 0):
+        for off in (1, 2, 3):
+            assert lib.svlm_cache_append(c, layer, vp(P), vp(P), vp(P), vp(P + off), 40) == ARG
+    assert ran() == [] and attend(c, 1) == ORDER                     # nothing was appended
+    assert lib.svlm_cache_append(c, 0, vp(P), vp(P), vp(P + 1), vp(P + 4), 40) == OK
+    ran()
+c = new()
+assert lib.svlm_qkv_append(c, 0, vp(P), vp(P), 128, 28, vp(P), vp(P + 2), 40, vp(P)) == ARG and ran() == []
+wide = new(hk=1, capacity=70000)
+assert append(wide, 40) == OK
+ran()
+for n, hq in ((40, 4), (1, 9)):
+    for kw in (dict(pos=P + 2), dict(Q=P + 1), dict(out=P + 1)):
+        assert attend(wide, n, hq=hq, **kw) == ARG
+assert ran() == []
+""")
