@@ -93,7 +93,17 @@ __device__ __forceinline__ uint2 ld_pair(const uint2* p) {
 }
 
 // A word of a record that meets its readers without a fence, a counter or a second round trip: { payload, tag }, 64 bits and so single-copy
-// atomic.  Nothing else is ever written to the area, the tag of a launch is its KV head's epoch + 1, and the epoch goes up by one per launch.
+// atomic.  Nothing else is ever written to the area, the tag of a launch is its KV head's epoch + 1, and the epoch goes up by one per launch: with the
+// last of the head's blocks to ask for it, so that no block of a launch, however late it begins and whoever has given up waiting for it, takes the
+// next launch's tag.  (It went up with the first block's last poll: a block that began after a wait had run out left records which
+// the next launch took for its own.)
+// (The answer is looked at when it is wanted, behind the outputs: looked at as soon as it has been asked for, it held up thread 0's queries by 0.13 us.)
+__device__ __forceinline__ unsigned long long ask_tag(unsigned long long* epoch) { return atomicAdd(epoch, 1ull); }      // { epoch, blocks that have asked }
+__device__ __forceinline__ unsigned tag_of(unsigned long long asked, unsigned long long* epoch, int splits) {
+    const unsigned tag = (unsigned)(asked >> 32) + 1;
+    if ((unsigned)asked == (unsigned)splits - 1) __stcg(epoch, (unsigned long long)tag << 32);      // nobody else asks before this launch has ended
+    return tag;
+}
 __device__ __forceinline__ void st_tagged2(void* p, unsigned a, unsigned b, unsigned tag) {
     const unsigned long long hi = (unsigned long long)tag << 32;
     asm volatile("st.relaxed.gpu.global.v2.b64 [%0], {%1, %2};" ::"l"(p), "l"(hi | a), "l"(hi | b) : "memory");
@@ -103,7 +113,7 @@ __device__ __forceinline__ void ld_tagged2(const void* p, unsigned long long& a,
 }
 template <int D>
 __host__ __device__ constexpr int tagged_rec_bytes() { return 8 * D * 4 + 8 * 16; }      // 8 columns of bf16 pairs, then (m, l) of each
-__host__ __device__ inline size_t tagged_head_bytes(int kv_heads) { return ((size_t)kv_heads * 4 + 127) & ~(size_t)127; }
+__host__ __device__ inline size_t tagged_head_bytes(int kv_heads) { return ((size_t)kv_heads * 8 + 127) & ~(size_t)127; }
 
 template <int D>
 struct R8 {
@@ -143,7 +153,7 @@ __device__ __forceinline__ int chunk_at(int row, int chunk) { return row * D + (
 // is written.  All thread blocks of the launch are resident together (one wave of them, and a dependent launch enters only when
 // all of them have passed their trigger), so the wait is for stragglers.
 template <int D>
-__device__ __forceinline__ void combine_tagged(int share, int shares, int splits, const unsigned char* parts, unsigned tag, unsigned* epoch, float* buf, int G,
+__device__ __forceinline__ void combine_tagged(int share, int shares, int splits, const unsigned char* parts, unsigned tag, float* buf, int G,
                                                uint16_t* out_row0, unsigned wait_limit, int* status) {
     constexpr int REC = tagged_rec_bytes<D>();
     const int groups = G * (D / 8), per = (groups + shares - 1) / shares;
@@ -250,7 +260,6 @@ __device__ __forceinline__ void combine_tagged(int share, int shares, int splits
         }
         if (g0 + 8 < per) __syncthreads();                   // the slabs are read before the next round writes them
     }
-    if (share == 0 && threadIdx.x == 0) __stcg(epoch, tag);  // every split's record has been seen, so everybody has read the epoch
     if (__builtin_expect(timed_out, 0)) atomicCAS(status, 0, -5);   // SVLM_ERR_TIMEOUT
 }
 
@@ -281,11 +290,11 @@ rows8_kernel(SvlmAttend8 a, int layer0, int n_layers, const uint16_t* Q, const i
     uint16_t q_lo[R8_TILES][PPL], q_hi[R8_TILES][PPL];
     int q_at[R8_TILES][PPL];
     uint16_t new_lo[2][PPL], new_hi[2][PPL];       // of the appended token's key, of its value
-    unsigned ep = 0;
-    unsigned* const epoch = reinterpret_cast<unsigned*>(vw.tagged) + hk;
+    unsigned long long asked = 0;                  // thread 0's
+    unsigned long long* const epoch = reinterpret_cast<unsigned long long*>(vw.tagged) + hk;
     auto axis_of = [&](int pair) { return a.rope_mode == 0 ? 0 : (pair < a.sec_t ? 0 : (pair < a.sec_th ? 1 : 2)); };
     auto load_queries = [&] {
-        if (LAYER && threadIdx.x == 0) ep = ld_l2(epoch);
+        if (LAYER && threadIdx.x == 0) asked = ask_tag(epoch);
 #pragma unroll
         for (int c = 0; c < R8_TILES; ++c) {
             const int m = m0 + c * R8_WARPS + warp, r = m < m_total ? m / G : 0, h = m < m_total ? m - r * G : 0;
@@ -502,7 +511,6 @@ rows8_kernel(SvlmAttend8 a, int layer0, int n_layers, const uint16_t* Q, const i
             sh.q_tok[col] = live ? m / G : -1;
         }
     }
-    if (threadIdx.x == 0) sh.tag = (int)(ep + 1);
     __syncthreads();
 
     float o[R8_TILES][C::KS][4];
@@ -941,6 +949,7 @@ rows8_kernel(SvlmAttend8 a, int layer0, int n_layers, const uint16_t* Q, const i
             }
         }
     }
+    if (LAYER && threadIdx.x == 0) sh.tag = (int)tag_of(asked, epoch, splits);
     __syncthreads();
     const int n_cols = min(C::COLS, m_total - m0);
     // (token r, head h) of column m lies at row r * q_heads + h = r * (q_heads - G) + m
@@ -986,7 +995,7 @@ rows8_kernel(SvlmAttend8 a, int layer0, int n_layers, const uint16_t* Q, const i
     if (LAYER) {
         const int groups = G * CH, shares = min((groups + R8_GROUPS - 1) / R8_GROUPS, splits);
         if (split < shares)
-            combine_tagged<D>(split, shares, splits, parts, (unsigned)sh.tag, epoch, merge, G, out + (q_row0 * q_heads + hk * G) * D, sh.wait_limit,
+            combine_tagged<D>(split, shares, splits, parts, (unsigned)sh.tag, merge, G, out + (q_row0 * q_heads + hk * G) * D, sh.wait_limit,
                               const_cast<int*>(&vw.ctrl->status));
         return;
     }

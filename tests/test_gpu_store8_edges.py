@@ -144,3 +144,32 @@ def test_large_scores_leave_the_size_of_the_output_alone(n, up):
     V = np.ones((1, 1, 2, 64)) * 1.75
     out = p.cache.decode_step(0, to_dev(K[0]), to_dev(V[0]), torch.zeros(1, dtype=torch.uint8, device="cuda"), torch.from_numpy(pos).cuda(), to_dev(Q))
     close(dev_to_f64(out), np.full((1, 8, 64), 1.75))
+
+
+@pytest.mark.parametrize("hq,hk", [(28, 4), (8, 2)])
+def test_steps_behind_one_that_gave_up_on_late_blocks(hq, hk):
+    """Steps that wait for nothing (no polls) beside another stream's matrix products, so that some of a launch's blocks begin when others
+    have given up on them: what those leave behind is not the next step's."""
+    p = Pair(700 + hq, hq=hq, hk=hk, d=128, sink=4, vw=3000, tw=400, capacity=4096)
+    p.append(p.rng.integers(0, 2, 2900))
+    work, side = torch.randn(4096, 4096, device="cuda", dtype=torch.bfloat16), torch.cuda.Stream()
+    into = torch.empty_like(work)
+    ty = torch.zeros(1, dtype=torch.uint8, device="cuda")
+
+    def step():
+        pos, K, V, Q = p.place([0]), p.normal(1, 1, hk, 128), p.normal(1, 1, hk, 128), bf16(p.rng.standard_normal((1, hq, 128)))
+        args = to_dev(K[0]), to_dev(V[0]), ty, torch.from_numpy(pos).cuda(), to_dev(Q)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            for _ in range(6):
+                torch.mm(work, work, out=into)
+        out = p.cache.decode_step(0, *args)
+        p.ref.append([0], pos, K, V)
+        return out, Q, pos
+    for _ in range(12):
+        p.cache.debug_set_wait_limit(0)
+        step()
+        p.cache.debug_set_wait_limit(1 << 20)
+        out, Q, pos = step()
+        close(dev_to_f64(out), p.ref.attend(0, Q, pos))
+    assert p.cache.status() == binding.ERR_TIMEOUT               # sticky
