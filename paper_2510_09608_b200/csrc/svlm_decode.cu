@@ -124,13 +124,14 @@ __host__ __device__ inline size_t ws_head_words(int layers, int kv_heads) {
 // { payload, tag } (the payload: two bf16 partial outputs, or a head's maximum or sum as fp32): a reader that
 // finds this launch's tag in a word has that word's payload, since an aligned 64-bit access is single-copy
 // atomic.  No fence, no counter and no second round trip stand between a CTA's stores and the combining CTAs'
-// loads.  Layout of the area: one epoch word per KV head (rounded up to 128 bytes), then per (KV head, split) a
+// loads.  Layout of the area: { epoch, CTAs that have asked } per KV head (rounded up to 128 bytes), then per (KV head, split) a
 // record { o[8][D] as 4 D words of 8 bytes, then per head (m, tag), (l, tag) }.  Nothing but tagged words is
 // ever written to the record part, the tag of a launch is its KV head's epoch + 1 and the epoch goes up by one
-// per launch, so a word left by an earlier launch never carries the current tag.
+// per launch, so a word left by an earlier launch never carries the current tag.  It goes up with the last of the head's CTAs to ask
+// for it: one that begins late, when others have given up waiting for it, does not take the next launch's tag.
 template <int D>
 __host__ __device__ constexpr int ll_rec_bytes() { return 8 * D * 4 + 8 * 16; }
-__host__ __device__ inline size_t ll_head_bytes(int kv_heads) { return ((size_t)kv_heads * 4 + 127) & ~(size_t)127; }
+__host__ __device__ inline size_t ll_head_bytes(int kv_heads) { return ((size_t)kv_heads * 8 + 127) & ~(size_t)127; }
 template <int D>
 __host__ __device__ constexpr int partial_floats() { return rec_bytes<D>() / 4; }
 
@@ -455,9 +456,7 @@ __device__ __forceinline__ void arrive_and_combine(int* s_last, unsigned* counte
 // by side in a record, the four lane groups of the six warps take 24 records at a time, two rounds in flight (one
 // record per lane with the lanes a record apart was 2 us slower: 32 cache lines per load instruction).  The four
 // record lanes meet through shuffles, the warps through `buf` (6 x 8 x 12 floats), and four threads per group
-// write the result.  Split 0, which by then has seen every split's record and therefore knows that every CTA of
-// the KV head has read the epoch, moves the epoch on for the next launch.  Called by all LAY_THREADS threads of the
-// first `shares` splits after a __syncthreads() that follows their last use of `buf`.
+// write the result.  Called by all LAY_THREADS threads of the first `shares` splits after a __syncthreads() that follows their last use of `buf`.
 // stamp: trace hook (stations 12, 15).
 constexpr int LAY_THREADS = DEC_CWARPS * 32;         // the per-layer kernel: consumer warps only (168 registers with two CTAs per SM)
 
@@ -468,7 +467,7 @@ __host__ __device__ inline int combine_shares(int groups, int splits) {
 
 template <int D, typename Stamp>
 __device__ __forceinline__ void combine_tagged(int share, int shares, int splits, const unsigned char* parts, unsigned tag,
-                                               unsigned* epoch, float* buf, int G, uint16_t* out_row0, unsigned wait_limit,
+                                               float* buf, int G, uint16_t* out_row0, unsigned wait_limit,
                                                int* status, Stamp stamp) {
     constexpr int REC = ll_rec_bytes<D>();
     const int groups = G * (D / 8);                          // groups of eight output elements
@@ -582,7 +581,6 @@ __device__ __forceinline__ void combine_tagged(int share, int shares, int splits
         }
         if (g0 + 8 < per) __syncthreads();   // the slabs are read before the next round writes them
     }
-    if (share == 0 && threadIdx.x == 0) __stcg(epoch, tag);
     if (__builtin_expect(timed_out, 0)) atomicCAS(status, 0, -5);   // SVLM_ERR_TIMEOUT
 }
 
@@ -1033,7 +1031,7 @@ decode_layer_kernel(SvlmAttendBatch b, int layer, const uint16_t* Q, const int* 
     const int n_rounds = (n_units + GROUP - 1) / GROUP;
     const size_t head_row0 = ((size_t)layer * b.kv_heads + hk) * b.n_slots;
     constexpr int REC = ll_rec_bytes<D>();
-    unsigned* epoch = reinterpret_cast<unsigned*>(records) + hk;
+    unsigned long long* epoch = reinterpret_cast<unsigned long long*>(records) + hk;
     unsigned char* ws_parts = records + ll_head_bytes(b.kv_heads) + (size_t)hk * splits * REC;   // this KV head's records
     unsigned char* part = ws_parts + (size_t)split * REC;                                       // 16-byte aligned
 
@@ -1143,10 +1141,10 @@ decode_layer_kernel(SvlmAttendBatch b, int layer, const uint16_t* Q, const int* 
             if (__builtin_expect(c <= -65536 || c >= 65536, 0)) f[e] = svlm_rope_cs(tab, HALF, pair, c, b.theta[pair]);
         }
     };
-    unsigned ep = 0;                                 // the KV head's epoch (same round trip as the query)
+    unsigned long long asked = 0;                    // thread 0's answer, looked at behind the outputs
     unsigned lo[HN], hi[HN], klo = 0, khi = 0, vlo = 0, vhi = 0;
     auto rows = [&] {                                // all loads first: one round trip
-        if (threadIdx.x == 0) ep = ld_l2(epoch);
+        if (threadIdx.x == 0) asked = atomicAdd(epoch, 1ull);
         auto two = [](const uint16_t* p) {           // two neighbouring elements
             return ANYWHERE ? (unsigned)ld_in(p) | (unsigned)ld_in(p + 1) << 16 : ld_in(reinterpret_cast<const unsigned*>(p));
         };
@@ -1207,7 +1205,6 @@ decode_layer_kernel(SvlmAttendBatch b, int layer, const uint16_t* Q, const int* 
             *reinterpret_cast<unsigned*>(sh.fresh + D + 2 * p2) = vlo;
             *reinterpret_cast<unsigned*>(sh.fresh + D + HALF + 2 * p2) = vhi;
         }
-        if (threadIdx.x == 0) sh.tag = (int)(ep + 1);
     }
     __syncthreads();
 #pragma unroll
@@ -1367,6 +1364,11 @@ decode_layer_kernel(SvlmAttendBatch b, int layer, const uint16_t* Q, const int* 
 #else
     auto stamp7 = [](int) {};
 #endif
+    if (threadIdx.x == 0) {
+        const unsigned tag = (unsigned)(asked >> 32) + 1;
+        sh.tag = (int)tag;
+        if ((unsigned)asked == (unsigned)splits - 1) __stcg(epoch, (unsigned long long)tag << 32);   // nobody else asks before this launch has ended
+    }
     cta_merge_and_record<D, true>(o, m, l, reinterpret_cast<float*>(ring), part, stamp7, &sh.tag);
     if constexpr (Append::on) {
         if (warp == DEC_CWARPS - 1) write_token_down(app, ci, sh.one, new_slot, before, gridDim.x * gridDim.y);
@@ -1385,7 +1387,7 @@ decode_layer_kernel(SvlmAttendBatch b, int layer, const uint16_t* Q, const int* 
 #else
     auto stamp = [](int) {};
 #endif
-    combine_tagged<D>(split, shares, splits, ws_parts, (unsigned)sh.tag, epoch, reinterpret_cast<float*>(ring), G,
+    combine_tagged<D>(split, shares, splits, ws_parts, (unsigned)sh.tag, reinterpret_cast<float*>(ring), G,
                       out + q_head0 * D, (unsigned)sh.wait_limit, const_cast<int*>(&vw.ctrl->status), stamp);
 #ifdef SVLM_DECODE_TRACE
     __syncthreads();

@@ -134,3 +134,34 @@ def test_projection_gives_up_and_recovers():
     assert t.cache.status() == binding.OK
     Q64 = qkv.project(X[:len(g2)], W, wl.q_heads, wl.kv_heads, wl.head_dim)[0]
     assert np.all(np.abs(dev_to_f64(Qg) - Q64) <= 2.0 ** -8 * np.abs(Q64) + 1e-5 * np.sqrt(hidden))
+
+
+def test_tokens_behind_one_that_gave_up_on_late_blocks():
+    """The per-layer decode kernel waiting for nothing beside another stream's matrix products, so that some of a launch's blocks begin when others
+    have given up on them: what those leave behind is not the next launch's."""
+    from harness import assert_close, bits_to_dev, dev_to_f64
+    from paper_2510_09608_b200 import binding, streamgen as sg
+    wl = dataclasses.replace(sg.workloads()[2], layers=1, n_sink=16, vision_window=2048, text_window=400, text_max=12, decode_steps=1)
+    s = _filled(wl, chunks=5)
+    work, side = torch.randn(4096, 4096, device="cuda", dtype=torch.bfloat16), torch.cuda.Stream()
+    into = torch.empty_like(work)
+
+    def token():
+        s.append_decode_token()
+        gids, _, pos = s.last
+        Qb = s.stream.q(0, gids)
+        Q, qp = bits_to_dev(Qb), torch.from_numpy(np.ascontiguousarray(pos)).cuda()
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            for _ in range(6):
+                torch.mm(work, work, out=into)
+        return s.cache.attend(0, Q, qp), Qb, pos
+    for _ in range(12):
+        s.cache.debug_set_wait_limit(0)
+        token()
+        s.cache.debug_set_wait_limit(1 << 20)
+        out, Qb, pos = token()
+        out = dev_to_f64(out)
+        s._give_values_to_ref(0)
+        assert_close(s._stats(out, s.ref.attend(0, Qb, pos)))
+    assert s.cache.status() == binding.ERR_TIMEOUT        # sticky
