@@ -418,7 +418,10 @@ int attend_common(svlm_cache* const* caches, int n_caches, int layer, const void
         SvlmAttend8 a;
         fill_attend8(caches, n_caches, a);
         int pages = 1;
-        for (int i = 0; i < n_caches; ++i) { pages = std::max(pages, expected_pages(caches[i])); if (!Knew) caches[i]->last_decode_layer = -1; }
+        for (int i = 0; i < n_caches; ++i) {
+            pages = std::max(pages, expected_pages(caches[i]));
+            if (!Knew) { caches[i]->last_decode_layer = -1; caches[i]->meta_settled = true; }      // (it lets nobody start before all earlier work is done)
+        }
         const int early = Knew && layer >= 0 && note_decode(caches, n_caches, layer) != 0;
         SVLM_CUDA(svlm_launch_rows8(a, {std::max(layer, 0), layer < 0 ? c0->dev.layers : 1, n_q, q_heads, Q, q_pos, out, pages, Knew, Vnew, early}, c0->stream));
         return SVLM_OK;
@@ -881,7 +884,7 @@ int svlm_attend_batched_varlen(svlm_cache* const* caches, int n_caches, int laye
         std::memcpy(a.q_off, b.q_off, sizeof a.q_off);
         std::memcpy(a.q_cnt, b.q_cnt, sizeof a.q_cnt);
         int pages = 1;
-        for (int i = 0; i < n_caches; ++i) pages = std::max(pages, expected_pages(caches[i]));
+        for (int i = 0; i < n_caches; ++i) { pages = std::max(pages, expected_pages(caches[i])); caches[i]->meta_settled = true; }
         SVLM_CUDA(svlm_launch_rows8(a, {layer, 1, n_max, q_heads, Q, q_pos, out, pages, nullptr, nullptr, 0}, c0->stream));
         return SVLM_OK;
     }

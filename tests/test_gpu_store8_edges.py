@@ -173,3 +173,45 @@ def test_steps_behind_one_that_gave_up_on_late_blocks(hq, hk):
         out, Q, pos = step()
         close(dev_to_f64(out), p.ref.attend(0, Q, pos))
     assert p.cache.status() == binding.ERR_TIMEOUT               # sticky
+
+
+@pytest.mark.parametrize("hq,hk,d,mrope", [(28, 4, 128, True), (8, 2, 64, False)])
+def test_short_chunks_layer_by_layer(hq, hk, d, mrope):
+    """Each layer's append directly behind the attention of the layer before it, as a model runs: few rows over the bytes, then a longer chunk, evictions
+    and generated tokens between them; one cache and two at a time, whose rows differ in number."""
+    ps = [Pair(800 + i, layers=3, hq=hq, hk=hk, d=d, sink=3, vw=120, tw=90, capacity=700, mrope=mrope) for i in range(2)]
+    for rnd, n in enumerate((9, 21, 200, 1, 33, 12)):
+        two = rnd % 3 == 1 or n == 12
+        new = []
+        for p in ps:
+            types = p.rng.integers(0, 2, n).astype(np.uint8)
+            pos = p.place(types)
+            K, V, Q = p.normal(3, n, hk, d), p.normal(3, n, hk, d), bf16(p.rng.standard_normal((3, n, hq, d)))
+            dev = to_dev(K), to_dev(V), to_dev(Q), torch.from_numpy(types).cuda(), torch.from_numpy(pos).cuda()
+            new.append((types, pos, K, V, Q, dev))
+        rows = [n, max(1, n - 3)]
+        outs = []
+        for l in range(3):
+            for p, (_, _, _, _, _, (k, v, q, ty, at)) in zip(ps, new):
+                p.cache.append(l, k[l], v[l], ty if l == 0 else None, at if l == 0 else None)
+                if not two:
+                    outs.append(p.cache.attend(l, q[l], at))
+            if two:
+                q = torch.cat([x[5][2][l][n - r:] for x, r in zip(new, rows)])
+                at = torch.cat([x[5][4][n - r:] for x, r in zip(new, rows)])
+                outs.append(binding.attend_batched_varlen([p.cache for p in ps], l, q, at, rows))
+        for p, (types, pos, K, V, Q, _) in zip(ps, new):
+            p.ref.append(types, pos, K, V)
+            assert p.cache.status() == binding.OK
+        for l in range(3):
+            for i, (p, (_, pos, _, _, Q, _)) in enumerate(zip(ps, new)):
+                if two:
+                    close(dev_to_f64(outs[l][sum(rows[:i]):sum(rows[:i + 1])]), p.ref.attend(l, Q[l][n - rows[i]:], pos[n - rows[i]:]))
+                else:
+                    close(dev_to_f64(outs[2 * l + i]), p.ref.attend(l, Q[l], pos))
+        for p in ps:
+            if rnd % 2:
+                p.evict()
+            p.check()
+            if hq // hk <= 8:
+                p.step()
