@@ -86,12 +86,6 @@ __device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commi
 template <int N>
 __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
-__device__ __forceinline__ uint2 ld_pair(const uint2* p) {
-    uint2 v;
-    asm volatile("ld.global.cg.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "l"(p) : "memory");
-    return v;
-}
-
 // A word of a record that meets its readers without a fence, a counter or a second round trip: { payload, tag }, 64 bits and so single-copy
 // atomic.  Nothing else is ever written to the area, the tag of a launch is its KV head's epoch + 1, and the epoch goes up by one per launch: with the
 // last of the head's blocks to ask for it, so that no block of a launch, however late it begins and whoever has given up waiting for it, takes the

@@ -387,7 +387,7 @@ int attend_common(svlm_cache* const* caches, int n_caches, int layer, const void
     if (q_heads % c0->dev.kv_heads) return SVLM_ERR_ARG;
     if (layer < -1 || layer >= c0->dev.layers) return SVLM_ERR_ARG;
     const int group = q_heads / c0->dev.kv_heads;
-    const bool split_kv = n_q == 1 && group <= 8 && svlm_decode_supported(c0->dev.n_pages);
+    const bool split_kv = !c0->bits8 && n_q == 1 && group <= 8 && svlm_decode_supported(c0->dev.n_pages);      // (8-bit caches have no scratch for it)
     const bool chunk = n_q >= 2 && svlm_prefill_supported(c0->dev.n_pages, group);
     if (list && !split_kv) return SVLM_ERR_ARG;      // (only the decode kernels append by themselves)
     const bool few8 = c0->bits8 && rows8(c0, n_q, q_heads);
@@ -548,7 +548,7 @@ int create(svlm_cache** out, int layers, int kv_heads, int head_dim, int n_sink,
         mem.add(&d.ev_gid[t], capacity);
         mem.add(&d.ev_pref[t], (size_t)capacity + 1);
     }
-    {   // split-KV scratch: the larger of a one-layer launch and an all-layers launch
+    if (!bits8) {   // split-KV scratch: the larger of a one-layer launch and an all-layers launch
         const size_t one = svlm_decode_ws_floats(layers, kv_heads, head_dim, svlm_decode_splits(d.n_pages, kv_heads, 1));
         const size_t all = svlm_decode_ws_floats(layers, kv_heads, head_dim, svlm_decode_splits(d.n_pages, kv_heads, layers));
         mem.add(&d.ws, std::max(one, all));

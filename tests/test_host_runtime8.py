@@ -53,3 +53,18 @@ for n, hq in ((40, 4), (1, 9)):
         assert attend(wide, n, hq=hq, **kw) == ARG
 assert ran() == []
 """)
+
+
+def test_device_memory_is_what_the_header_lists(host):  # noqa: F811
+    """28 layers of 4 heads of 128 fit into the parts that include/svlm.h names and 128 bytes a token for the metadata; no scratch of kernels that an
+    8-bit cache never takes (9 MB here)."""
+    host(NEW8 + """
+L, H, D, capacity, sink = 28, 4, 128, 9800, 512
+slots = 128 * ((sink + 127) // 128 + (capacity + 127) // 128 + 4)
+bytes8 = 2 * L * H * slots * D + 4 * L * H * slots // 16
+widened, turns, table = 2 * H * slots * D * 2, 2 * D * slots, 12 * 1024 * D // 2
+fake.fake_alloc_limit(bytes8 + widened + turns + table + (3 << 20) + 128 * slots)
+c = new8(L, H, D, sink, 8192, 512, capacity)
+assert append(c, 40, layer=-1) == OK and step(c) == OK and attend(c, 1) == OK and attend(c, 1, hq=36) == OK and attend(c, 41) == OK
+assert not any("decode" in k for k in ran())
+""")
