@@ -390,6 +390,13 @@ int attend_common(svlm_cache* const* caches, int n_caches, int layer, const void
     const bool split_kv = !c0->bits8 && n_q == 1 && group <= 8 && svlm_decode_supported(c0->dev.n_pages);      // (8-bit caches have no scratch for it)
     const bool chunk = n_q >= 2 && svlm_prefill_supported(c0->dev.n_pages, group);
     if (list && !split_kv) return SVLM_ERR_ARG;      // (only the decode kernels append by themselves)
+    for (int i = 0; i < n_caches; ++i) {
+        svlm_cache* c = caches[i];
+        if (!c || !same_geometry(c, c0)) return SVLM_ERR_ARG;
+        if (n_q > c->appended) return SVLM_ERR_ORDER;
+        note_capture(c);
+    }
+    DeviceGuard guard(c0->device);
     const bool few8 = c0->bits8 && rows8(c0, n_q, q_heads);
     if (c0->bits8 && !few8 && layer < 0 && c0->dev.layers > 1) {      // widened and attended layer by layer
         const size_t rows = (size_t)n_caches * n_q * q_heads * c0->dev.head_dim;
@@ -405,15 +412,7 @@ int attend_common(svlm_cache* const* caches, int n_caches, int layer, const void
     SvlmAttendBatch b;
     b.n_caches = n_caches;
     fill_batch_geometry(c0, b);
-    for (int i = 0; i < n_caches; ++i) {
-        svlm_cache* c = caches[i];
-        if (!c) return SVLM_ERR_ARG;
-        if (!same_geometry(c, c0)) return SVLM_ERR_ARG;
-        if (n_q > c->appended) return SVLM_ERR_ORDER;
-        note_capture(c);
-        fill_view(c, b.view[i]);
-    }
-    DeviceGuard guard(c0->device);
+    for (int i = 0; i < n_caches; ++i) fill_view(caches[i], b.view[i]);
     if (few8) {
         SvlmAttend8 a;
         fill_attend8(caches, n_caches, a);

@@ -68,3 +68,18 @@ c = new8(L, H, D, sink, 8192, 512, capacity)
 assert append(c, 40, layer=-1) == OK and step(c) == OK and attend(c, 1) == OK and attend(c, 1, hq=36) == OK and attend(c, 41) == OK
 assert not any("decode" in k for k in ran())
 """)
+
+
+def test_a_captured_attention_is_reckoned_with_full_windows(host):  # noqa: F811
+    """The attention call alone in a graph, captured on a nearly empty cache: its kernels are those of full windows already in that call."""
+    host(NEW8 + """
+c = new8(vw=8192, tw=512, capacity=9800)
+assert append(c, 200) == OK
+ran()
+assert attend(c, 40) == OK
+assert any("rows8" in k for k in ran())
+fake.fake_capturing(1)
+assert attend(c, 40) == OK
+got = ran()
+assert any("widen8" in k for k in got) and not any("rows8" in k for k in got), got
+""")
