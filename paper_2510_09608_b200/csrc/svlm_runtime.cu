@@ -348,16 +348,36 @@ int note_decode(svlm_cache* const* caches, int n_caches, int layer) {
 }
 
 // Few rows go over the 8-bit cache as it is (svlm_rows8.cu), whose time grows with rows times keys, more over a layer widened to bf16, whose time hardly
-// depends on the rows here.  Rows of a KV head (4 KV heads of 128, one cache) where the two are alike: about 105 over 9216 keys (43 us), 175 over 3100 (33),
-// 500 over 336 (25).  Measured on both sides, us: 63 rows over 9216 keys 30 and 45, 126 49 and 44; over 3100 keys 126 rows 27 and 34, 252 42 and 35;
-// over 336 keys 252 rows 14 and 23, 700 32 and 25.  Beyond the chunk kernel's list of pages what is left for many rows is the general kernel: 63 rows
+// depends on the rows here.  One cache: rows of a KV head (4 KV heads of 128) where the two are alike: about 105 over 9216 keys (43 us), 175 over 3100 (33),
+// 500 over 336 (25).  Measured on both sides, us: 63 rows over 9216 keys 27 and 42, 126 45 and 42; over 3100 keys 126 rows 23 and 33, 252 34 and 33;
+// over 336 keys 252 rows 13 and 25, 511 19 and 25.  Beyond the chunk kernel's list of pages what is left for many rows is the general kernel: 63 rows
 // over 44512 keys 112 us and 10.7 ms.
+// Several caches and many KV heads: what is latency for one is throughput for them, and the two times are reckoned (us).  Over the bytes: 9, the
+// bytes once for each 8 rows, and 12 for each further wave of thread blocks, of which 296 are resident.  Widened: 21 to 29, the widening, and the chunk kernel's
+// tiles of 256 rows.  Measured on both sides, 28/4 heads of 128, 16 caches: over 9216 keys 28 rows 142 and 200, 63 276 and 201; over 336 keys 28 rows 15 and
+// 28, 252 105 and 30; 16/8 heads of 64, four caches over 3100 keys: 32 rows 26 and 38, 128 87 and 38; 32/8 of 128, one cache over 9216: 64 rows 45 and 48, 128 78 and 48.
+// Over 414 such shapes (7 head shapes, 1, 4 and 16 caches) both conditions together are 1.5 % behind the better side; the first alone 10 %, up to 7 times.
 constexpr long long ROWS8_MOST = 1 << 20, ROWS8_KEYS = 2560;
-bool rows8(const svlm_cache* c, int n_q, int q_heads) {
-    const int group = q_heads / c->dev.kv_heads;
+// each: rows of each cache, or null: n_q of all.  layers: of the launch
+bool rows8(svlm_cache* const* caches, int n_caches, int layers, int n_q, const int32_t* each, int q_heads) {
+    const svlm_cache* c0 = caches[0];
+    const int kv_heads = c0->dev.kv_heads, group = q_heads / kv_heads;
     const long long rows = (long long)n_q * group;
-    if (!svlm_rows8_supported(c->dev.n_pages) || (rows + 7) / 8 * c->dev.kv_heads > 65535) return false;
-    return n_q == 1 || !svlm_prefill_supported(c->dev.n_pages, group) || rows * ((long long)expected_pages(c) * SVLM_PAGE + ROWS8_KEYS) <= ROWS8_MOST;
+    if (!svlm_rows8_supported(c0->dev.n_pages) || (rows + 7) / 8 * kv_heads > 65535) return false;
+    if (n_q == 1 || !svlm_prefill_supported(c0->dev.n_pages, group)) return true;
+    const double heads = (double)layers * kv_heads, wide = c0->dev.head_dim / 128.0;
+    double blocks = 0, bytes = 0, widened = 0;
+    long long most_keys = 0;
+    for (int i = 0; i < n_caches; ++i) {
+        const long long mine = (long long)(each ? each[i] : n_q) * group, keys = (long long)expected_pages(caches[i]) * SVLM_PAGE;
+        most_keys = std::max(most_keys, keys);
+        blocks += heads * ((mine + 7) / 8);
+        bytes += heads * ((mine + 7) / 8) * keys;
+        widened += heads * keys * wide * (150 + 130 * ((mine + 255) / 256));
+    }
+    const double over_bytes = 9 + 12 * std::max(0.0, blocks / (2 * svlm_sm_count()) - 1) + bytes * (33 + 24 * wide) * 1e-6;
+    const double over_widened = layers * (21 + std::min<long long>(most_keys, 4096) / 512.0) + widened * 1e-6;
+    return rows * (most_keys + ROWS8_KEYS) <= ROWS8_MOST && over_bytes <= over_widened;
 }
 
 void fill_attend8(svlm_cache* const* caches, int n_caches, SvlmAttend8& a) {
@@ -397,7 +417,7 @@ int attend_common(svlm_cache* const* caches, int n_caches, int layer, const void
         note_capture(c);
     }
     DeviceGuard guard(c0->device);
-    const bool few8 = c0->bits8 && rows8(c0, n_q, q_heads);
+    const bool few8 = c0->bits8 && rows8(caches, n_caches, layer < 0 ? c0->dev.layers : 1, n_q, nullptr, q_heads);
     if (c0->bits8 && !few8 && layer < 0 && c0->dev.layers > 1) {      // widened and attended layer by layer
         const size_t rows = (size_t)n_caches * n_q * q_heads * c0->dev.head_dim;
         for (int l = 0; l < c0->dev.layers; ++l) {
@@ -470,7 +490,7 @@ int decode_step8(const SvlmCacheList& list, svlm_cache* const* caches, int n_cac
                                 : svlm_launch_append_meta_batch(list, c0->dev, token_type, pos, 1, c0->stream));
         for (int i = 0; i < n_caches; ++i) note_append(caches[i], 1);
     }
-    if (rows8(c0, 1, q_heads)) return attend_common(caches, n_caches, layer, Q, pos, 1, q_heads, out, K, V);
+    if (rows8(caches, n_caches, 1, 1, nullptr, q_heads)) return attend_common(caches, n_caches, layer, Q, pos, 1, q_heads, out, K, V);
     const size_t row = (size_t)c0->dev.kv_heads * c0->dev.head_dim, axes = c0->dev.rope_mode == SVLM_ROPE_1D ? 1 : 3;
     for (int i = 0; i < n_caches; ++i)
         SVLM_CUDA(svlm_launch_kv_write8(caches[i]->dev, caches[i]->store8, layer, static_cast<const uint16_t*>(K) + i * row,
@@ -876,7 +896,7 @@ int svlm_attend_batched_varlen(svlm_cache* const* caches, int n_caches, int laye
     }
     if (off > 0x7fffffffll) return SVLM_ERR_ARG;
     DeviceGuard guard(c0->device);
-    if (c0->bits8 && rows8(c0, n_max, q_heads)) {
+    if (c0->bits8 && rows8(caches, n_caches, 1, n_max, n_q, q_heads)) {
         SvlmAttend8 a;
         fill_attend8(caches, n_caches, a);
         a.q_varlen = 1;

@@ -83,3 +83,47 @@ assert attend(c, 40) == OK
 got = ran()
 assert any("widen8" in k for k in got) and not any("rows8" in k for k in got), got
 """)
+
+
+def test_few_rows_or_a_widened_layer(host):  # noqa: F811
+    """Which way a chunk goes over one cache and over several, of one length and of several; both sides were measured at each of these (us, bytes and widened)."""
+    host(NEW8 + """
+def fill(n, hk, d, keys, hq):
+    cs = [new8(2, hk, d, 4, keys - 68, 64, keys + 600) for _ in range(n)]
+    for c in cs:
+        for at in range(0, keys, 512):
+            assert append(c, min(512, keys - at), layer=-1) == OK
+    return cs
+
+def way(call):
+    ran()
+    assert call() == OK
+    got = ran()
+    few = any("rows8" in k for k in got)
+    assert few != any("widen8" in k for k in got), got
+    return few
+
+for streams, hq, hk, d, keys, n, few in (
+        (1, 28, 4, 128, 9216, 9, True), (1, 28, 4, 128, 9216, 73, False),           # 27 and 42, 141 and 43
+        (4, 28, 4, 128, 9216, 4, True), (4, 28, 4, 128, 9216, 18, False),           # 45 and 73, 141 and 73
+        (16, 28, 4, 128, 9216, 4, True), (16, 28, 4, 128, 9216, 9, False),          # 142 and 201, 276 and 201
+        (16, 28, 4, 128, 336, 4, True), (16, 28, 4, 128, 336, 36, False),           # 15 and 28, 105 and 30
+        (4, 16, 8, 64, 3100, 16, True), (4, 16, 8, 64, 3100, 64, False),            # 26 and 38, 87 and 38
+        (1, 32, 8, 128, 9216, 16, True), (1, 32, 8, 128, 9216, 32, False),          # 45 and 48, 78 and 48
+        (16, 4, 1, 64, 9216, 8, True), (16, 4, 1, 64, 9216, 32, False)):            # 35 and 49, 110 and 49
+    cs = fill(streams, hk, d, keys, hq)
+    one = lambda: attend(cs[0], n, hq=hq) if streams == 1 else lib.svlm_attend_batched(arr(cs), streams, 1, vp(P), vp(P), n, hq, vp(P))
+    assert way(one) == few, (streams, hq, hk, d, keys, n)
+    each = (C.c_int32 * streams)(*[n] * streams)
+    assert way(lambda: lib.svlm_attend_batched_varlen(arr(cs), streams, 1, vp(P), vp(P), each, hq, vp(P))) == few
+    for c in cs:
+        lib.svlm_cache_destroy(c)
+
+# sixteen caches one of which has a question of nine tokens, the others one token each; 28 layers in one call
+cs = fill(16, 4, 128, 9216, 28)
+each = (C.c_int32 * 16)(9, *[1] * 15)
+assert way(lambda: lib.svlm_attend_batched_varlen(arr(cs), 16, 1, vp(P), vp(P), each, 28, vp(P)))
+assert way(lambda: attend(cs[0], 9, layer=-1)) and not way(lambda: attend(cs[0], 73, layer=-1))
+# an array with a hole in it is refused, not read
+assert lib.svlm_attend_batched((vp * 2)(cs[0], None), 2, 0, vp(P), vp(P), 4, 28, vp(P)) == ARG
+""")
