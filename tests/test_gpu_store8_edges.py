@@ -12,15 +12,18 @@ from test_gpu_store8 import Pair, close, to_dev
 pytestmark = pytest.mark.gpu
 
 
-def batched_step(ps, check=True):
-    """One generated token of every stream through all layers, in lock step."""
+def batched_step(ps, between=lambda out: None):
+    """One generated token of every stream through all layers, in lock step; `between` gets each layer's output."""
     layers, hq, hk, d, n = ps[0].L, ps[0].hq, ps[0].hk, ps[0].d, len(ps)
     pos = np.stack([p.place([0]) for p in ps]).reshape(n)
     K, V = [p.normal(layers, 1, hk, d) for p in ps], [p.normal(layers, 1, hk, d) for p in ps]
     Q = bf16(ps[0].rng.standard_normal((layers, n, hq, d)))
     ty, qp = torch.zeros(n, dtype=torch.uint8, device="cuda"), torch.from_numpy(pos).cuda()
     k, v, q = ([to_dev(np.stack([x[l, 0] for x in xs])) for l in range(layers)] for xs in (K, V, [Q[:, None, i] for i in range(n)]))
-    outs = [binding.decode_step_batched([p.cache for p in ps], l, k[l], v[l], ty if l == 0 else None, qp, q[l]) for l in range(layers)]
+    outs = []
+    for l in range(layers):
+        outs.append(binding.decode_step_batched([p.cache for p in ps], l, k[l], v[l], ty if l == 0 else None, qp, q[l]))
+        between(outs[-1])
     for i, p in enumerate(ps):
         p.ref.append([0], pos[i:i + 1], K[i], V[i])
         for l in range(layers):
@@ -215,3 +218,78 @@ def test_short_chunks_layer_by_layer(hq, hk, d, mrope):
             p.check()
             if hq // hk <= 8:
                 p.step()
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_two_chains_on_two_streams(d):
+    """Generated tokens of two caches through all their layers, on a CUDA stream each and without a synchronisation between them: the blocks in which a
+    launch's parts meet wait for others of theirs while another chain's launches take places on the GPU."""
+    ps = [Pair(900 + i, layers=6, hq=8, hk=2, d=d, sink=4, vw=1500, tw=300, capacity=2200) for i in range(2)]
+    streams = [torch.cuda.Stream() for _ in ps]
+    for p in ps:
+        p.append(p.rng.integers(0, 2, 1600))
+        p.evict()
+    torch.cuda.synchronize()
+    ty = torch.zeros(1, dtype=torch.uint8, device="cuda")
+    steps = []
+    for _ in range(8):
+        for p in ps:
+            pos = p.place([0])
+            K, V, Q = p.normal(6, 1, 2, d), p.normal(6, 1, 2, d), bf16(p.rng.standard_normal((6, 1, 8, d)))
+            steps.append((p, pos, K, V, Q, to_dev(K), to_dev(V), to_dev(Q), torch.from_numpy(pos).cuda(), torch.empty(6, 1, 8, d, dtype=torch.bfloat16, device="cuda")))
+    torch.cuda.synchronize()
+    for p, s in zip(ps, streams):
+        p.cache.set_stream(s)
+    for l in range(0, len(steps), 2):                        # a launch of the one, a launch of the other
+        for layer in range(6):
+            for p, _, _, _, _, k, v, q, at, out in steps[l:l + 2]:
+                p.cache.decode_step(layer, k[layer], v[layer], ty if layer == 0 else None, at, q[layer], out[layer])
+    torch.cuda.synchronize()
+    for p, pos, K, V, Q, *_, out in steps:
+        p.ref.append([0], pos, K, V)
+        for layer in range(6):
+            close(dev_to_f64(out[layer]), p.ref.attend(layer, Q[layer], pos))
+    for p in ps:
+        assert p.cache.status() == binding.OK
+        p.cache.set_stream(torch.cuda.current_stream())
+        p.check()
+
+
+def test_batched_steps_with_projections_between_the_layers():
+    """The layers' launches of a batched step begin early, but not as a chain: 4-bit projections of each layer's output run between them, as in a
+    decoder.  (What is projected goes nowhere: the next layer's inputs are of the size that the tolerances are derived for.)"""
+    import test_gpu_w4 as w4
+    ps = [Pair(920 + i, layers=3, hq=8, hk=2, d=128, sink=4, vw=200, tw=100, capacity=700) for i in range(3)]
+    for i, p in enumerate(ps):
+        p.append(p.rng.integers(0, 2, 150 + 70 * i))
+        p.evict()
+    _, w, s = w4.inputs(3, 1024, 1536, 128, 5)
+    for _ in range(4):
+        batched_step(ps, between=lambda out: ps[0].cache.proj_w4(out.view(3, 1024), w, s))
+    for p in ps:
+        p.check()
+
+
+@pytest.mark.parametrize("n_q", [[3, 3, 3], [9, 9, 9], [2, 40, 7]])
+def test_batched_short_chunks_over_full_caches(n_q):
+    """Questions of three streams over thousands of keys, of one length and of several: over the bytes and, by the number of rows and caches, over
+    widened layers."""
+    ps = [Pair(940 + i, hq=28, hk=4, d=128, sink=64, vw=3000, tw=300, capacity=3700, mrope=True, base=1e6) for i in range(3)]
+    for p, n in zip(ps, n_q):
+        p.append(np.r_[np.zeros(200), np.ones(2900)])
+        p.append(np.r_[np.ones(300), np.zeros(60)])
+        p.evict()
+        p.append([0] * n)
+    Q = [bf16(p.rng.standard_normal((n, 28, 128))) for p, n in zip(ps, n_q)]
+    pos = torch.from_numpy(np.ascontiguousarray(np.concatenate([p.pos for p in ps]))).cuda()
+    q, caches = to_dev(np.concatenate(Q)), [p.cache for p in ps]
+    if len(set(n_q)) == 1:
+        n = n_q[0]
+        got = dev_to_f64(binding.attend_batched(caches, 0, q.view(3, n, 28, 128), pos.view(3, n, 3))).reshape(-1, 28, 128)
+    else:
+        got = dev_to_f64(binding.attend_batched_varlen(caches, 0, q, pos, n_q))
+    at = 0
+    for p, n, x in zip(ps, n_q, Q):
+        assert p.cache.status() == binding.OK
+        close(got[at:at + n], p.ref.attend(0, x, p.pos))
+        at += n
