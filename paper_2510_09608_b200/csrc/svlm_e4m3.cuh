@@ -11,6 +11,8 @@ constexpr float E8_TOP = 240.f;                 // the largest value in units of
 
 __device__ __forceinline__ float pow2i(int e) { return __int_as_float((127 + e) << 23); }      // -126 <= e <= 127
 
+constexpr unsigned NO_EXPONENTS = (unsigned)(E8_MIN & 255) * 0x101u;     // of a block that holds nothing
+
 // Of a block's keys (0) or values (1).
 __device__ __forceinline__ int exponent_of(unsigned exps, int which) { return (int)(exps << (24 - 8 * which)) >> 24; }
 

@@ -121,6 +121,10 @@ __global__ void __launch_bounds__(SVLM_BLOCK8 * D / 16) kv_write8_kernel(SvlmCac
             if (tid == 0) st.apart[base / T] = before == 0 ? 0 : MIXED8;
         }
         enter();
+        // A block that begins: the layers that are still to come have nothing in it yet.  (An eviction behind layer 0's append looks at their exponents,
+        // and what a page's earlier tokens have left there may be 2^100 above everything.)
+        if (layer == 0 && blockIdx.y == 0 && !any_old)
+            for (int r = cd.kv_heads + tid; r < cd.layers * cd.kv_heads; r += THREADS) st.exps[((size_t)r * cd.n_slots + base) / T] = NO_EXPONENTS;
         for (int r = row0; r < row1; ++r) {
             const int l = r / cd.kv_heads, h = r - l * cd.kv_heads;
             const size_t row = (size_t)(first_row + r) * cd.n_slots, src = (((size_t)l * n + (fresh ? gid - first : 0)) * cd.kv_heads + h) * D + g * 8;

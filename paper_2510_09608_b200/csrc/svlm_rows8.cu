@@ -584,6 +584,9 @@ rows8_kernel(SvlmAttend8 a, int layer0, int n_layers, const uint16_t* Q, const i
                 vw.native[new_slot] = ld_l2(vw.slot_c + new_slot) + S;
             }
             if (apart != 0 && lane < D / 4) vw.turn[(size_t)new_slot * (D / 4) + lane] = make_uint2(0x3c003c00u, 0u);
+            if (held == 0 && n_layers == 1)        // the block begins: later layers have nothing in it yet (kv_write8_kernel)
+#pragma unroll 1
+                for (int row = a.kv_heads + lane; row < a.layers * a.kv_heads; row += 32) vw.exps[((size_t)row * a.n_slots + first) / SVLM_BLOCK8] = NO_EXPONENTS;
         }
         __syncwarp();
         return result;

@@ -293,3 +293,31 @@ def test_batched_short_chunks_over_full_caches(n_q):
         assert p.cache.status() == binding.OK
         close(got[at:at + n], p.ref.attend(0, x, p.pos))
         at += n
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("up", [0, -70])
+def test_a_giant_in_a_page_that_is_used_again(d, up):
+    """The second layer's keys of new tokens arrive when the eviction is over; their page is one that a key of 1e30 (or ordinary ones, among keys that are far
+    smaller since) has left.  What lies there of it is nobody's unit."""
+    p = Pair(960, layers=2, hq=8, hk=2, d=d, sink=0, vw=200, tw=64, capacity=700)
+    n = 130
+    for rnd in range(5):
+        types = np.ones(n, np.uint8)
+        pos = p.place(types)
+        K, V = bf16(p.normal(2, n, 2, d) * 2.0 ** (up if rnd else 0)), p.normal(2, n, 2, d)
+        if rnd == 0:
+            K[1, 5] = bf16(K[1, 5] * 1e30)
+        p.cache.append(0, to_dev(K[0]), to_dev(V[0]), torch.from_numpy(types).cuda(), torch.from_numpy(pos).cuda())
+        p.ref.append_meta(types, pos)
+        p.ref.write(0, K[0], V[0])
+        p.evict()
+        p.cache.append(1, to_dev(K[1]), to_dev(V[1]))
+        p.ref.write(1, K[1], V[1])
+        if rnd < 2:                                          # (the giant is there)
+            continue
+        for n_q in (n, 3):
+            Q = bf16(p.rng.standard_normal((n_q, 8, d)) * 2.0 ** -up)
+            got = dev_to_f64(p.cache.attend(1, to_dev(Q), torch.from_numpy(np.ascontiguousarray(pos[-n_q:])).cuda()))
+            close(got, p.ref.attend(1, Q, pos[-n_q:]))
+    p.check()
