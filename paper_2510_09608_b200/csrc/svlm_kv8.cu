@@ -283,8 +283,8 @@ __global__ void __launch_bounds__(256) shift8_kernel(SvlmCacheList list, SvlmSto
 // One thread block per (page, KV head); a thread has 8 pairs of four tokens, which usually share their rotation (what follows the last
 // evicted token shares one shift), so its factors are looked up once.  early: as above, the kernel before this one writes none of the cache's metadata (but
 // may write this layer's bytes).  half: the unit of a head's keys is kept with the bytes (SvlmStore8::most).  Where a block that has lost tokens
-// owes its unit to one of them, it may be 2^20 above that (see shift8_kernel); what does not fit f16 then is held at its largest value: a
-// key that far above all others decides its rows' softmax either way.
+// owes its unit to one of them, it may be 2^20 above that (see shift8_kernel); what is more than 2^6 above then (448 sqrt(2) 2^6 is a half) is held as
+// 2^6 above: a key that is 2^26 times all other blocks' decides its rows' softmax either way, by the sign of its score, which its direction gives.
 // One layer of 10,000 tokens of 4 heads of 128: 9 us, 31 MB; 20 with a thread's four heads one after another and the unit found by each thread block for itself.
 template <int D, bool HALF_KEYS>
 __device__ __forceinline__ void widen8(const SvlmCacheDev& cd, const SvlmStore8& st, int layer, int early) {
@@ -338,13 +338,9 @@ __device__ __forceinline__ void widen8(const SvlmCacheDev& cd, const SvlmStore8&
     for (int i = 0; i < TOKENS; ++i) {
         if (live[i] && by[i] != turned) factors(by[i]);
         const int up = exponent_of(exps[i], 0) - unit;       // (f16: 0 at most, but for the case above)
-        const float ku = pow2i(max(-126, min(127, up))), vu = pow2i(exponent_of(exps[i], 1));
+        const float ku = pow2i(max(-126, min(HALF_KEYS ? 6 : 127, up))), vu = pow2i(exponent_of(exps[i], 1));
         auto key = [&](float p, float q) {
             if (HALF_KEYS) {
-                if (__builtin_expect(up > 6, 0)) {
-                    if (p == p) p = fminf(fmaxf(p, -65504.f), 65504.f);
-                    if (q == q) q = fminf(fmaxf(q, -65504.f), 65504.f);
-                }
                 const __half2 y = __floats2half2_rn(p, q);
                 return *reinterpret_cast<const unsigned*>(&y);
             }

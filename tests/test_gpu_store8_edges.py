@@ -321,3 +321,24 @@ def test_a_giant_in_a_page_that_is_used_again(d, up):
             got = dev_to_f64(p.cache.attend(1, to_dev(Q), torch.from_numpy(np.ascontiguousarray(pos[-n_q:])).cuda()))
             close(got, p.ref.attend(1, Q, pos[-n_q:]))
     p.check()
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("by", [1e8, 1e12, 1e30])
+def test_a_giant_that_stays_when_another_has_left_its_block(d, by):
+    """Two keys that are `by` times all others in one block, of which one is evicted: the other has all the weight of the queries it agrees with and none of
+    the others', though its parts are far beyond f16 in the others' units.  (Its two directions turn with the position by 0.02 at most, and
+    q.k is 0.8 or -0.8 of `by` before the rotation.)"""
+    p = Pair(980, hq=8, hk=2, d=d, sink=0, vw=20, tw=400, capacity=768)
+    K = p.normal(1, 190, 2, d)
+    K[0, 3], K[0, 12] = bf16(K[0, 3] * by), 0
+    K[0, 12, :, d // 2 - 1], K[0, 12, :, d // 2 - 2] = bf16(by), bf16(-0.1 * by)
+    p.append([1] * 30 + [0] * 160, K=K)
+    p.evict()
+    p.check()
+    for n_q in (1, 5, 140):
+        Q, pos = bf16(p.rng.standard_normal((n_q, 8, d))), p.pos[-n_q:]
+        sign = np.where(p.rng.integers(0, 2, (n_q, 8)), 1.0, -1.0)
+        Q[..., d // 2 - 1], Q[..., d // 2 - 2] = sign, 2 * sign
+        got = dev_to_f64(p.cache.attend(0, to_dev(Q), torch.from_numpy(np.ascontiguousarray(pos)).cuda()))
+        close(got, p.ref.attend(0, Q, pos))
