@@ -82,8 +82,7 @@ int svlm_cache_create(svlm_cache** out, int layers, int kv_heads, int head_dim, 
  * largest.  Keys are rotated at their NATIVE position before the rounding (sines and cosines rounded to fp32, then two products and a sum in
  * fp32, each rounded) and are not touched again: attention
  * turns the query by what evictions have shifted a token.  NaN and infinities are stored as NaN in their own place; they show in the rows that
- * see them.  (Where a chunk has so many rows that it goes over a widened layer, a value of its own tokens that is not finite also shows in the rows of
- * tokens of its page that come before it.)
+ * see them, values in their own dims.
  * Device memory: the 8-bit slabs with 4 bytes of exponents per 16 tokens and head; one layer's K and V in bf16 in which long chunks see the cache
  * (2 x [kv_heads][pages*128][head_dim]); 2 x head_dim bytes a token of rotation factors that evictions leave; the rotation table in 64 bits
  * (12 KB x head_dim / 2) and some 3 MB in which a launch's parts meet.

@@ -35,6 +35,8 @@ __device__ __forceinline__ uint16_t to_e4m3x2(float lo, float hi, float limit = 
     asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
     return r;
 }
+// Of a word's four bytes those that are NaN (0x7f, 0xff): their lowest bits.
+__device__ __forceinline__ unsigned nan_bytes(unsigned w) { return (((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) >> 7; }
 // Two bytes as two halves (exact).
 __device__ __forceinline__ unsigned e4m3x2_to_half2(uint16_t x) {
     unsigned r;

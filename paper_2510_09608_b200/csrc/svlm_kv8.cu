@@ -17,6 +17,9 @@ namespace {
 __device__ __forceinline__ int axis_of(const SvlmCacheDev& cd, int pair) {
     return cd.rope_mode == 0 ? 0 : (pair < cd.sec_t ? 0 : (pair < cd.sec_th ? 1 : 2));
 }
+__device__ __forceinline__ SvlmHead8* heads_of(const SvlmCacheDev& cd) {
+    return reinterpret_cast<SvlmHead8*>(static_cast<unsigned char*>(cd.tmaps) + 512);
+}
 // Factors of pairs 8 g .. 8 g + 7 at positions p; a short loop, since this is code that runs once.
 __device__ __forceinline__ void factors8(const SvlmCacheDev& cd, int g, const int (&p)[3], float2 (&cs)[8]) {
     const float2* tab = reinterpret_cast<const float2*>(cd.rope_tab);
@@ -248,7 +251,10 @@ __global__ void __launch_bounds__(256) shift8_kernel(SvlmCacheList list, SvlmSto
         whole = __reduce_max_sync(0xffffffffu, whole);
         if ((threadIdx.x & 31) == 0) { atomicMax(&s_all, all); atomicMax(&s_whole, whole); }
         __syncthreads();
-        if (threadIdx.x == 0) stores.at[blockIdx.y].most[row] = (s_whole == E8_MIN ? s_all : min(s_all, s_whole + 20)) + MOST8_BIAS;
+        if (threadIdx.x == 0) {
+            stores.at[blockIdx.y].most[row] = (s_whole == E8_MIN ? s_all : min(s_all, s_whole + 20)) + MOST8_BIAS;
+            if (row < cd.kv_heads) heads_of(cd)[row].late = 0;
+        }
         return;
     }
     if ((int)blockIdx.x >= n_tiles) return;
@@ -287,7 +293,7 @@ __global__ void __launch_bounds__(256) shift8_kernel(SvlmCacheList list, SvlmSto
 // 2^6 above: a key that is 2^26 times all other blocks' decides its rows' softmax either way, by the sign of its score, which its direction gives.
 // One layer of 10,000 tokens of 4 heads of 128: 9 us, 31 MB; 20 with a thread's four heads one after another and the unit found by each thread block for itself.
 template <int D, bool HALF_KEYS>
-__device__ __forceinline__ void widen8(const SvlmCacheDev& cd, const SvlmStore8& st, int layer, int early) {
+__device__ __forceinline__ void widen8(const SvlmCacheDev& cd, const SvlmStore8& st, int layer, int n_q, int early) {
     using namespace svlm_ptx;
     constexpr int HALF = D / 2, GROUPS = HALF / 8, TOKENS = 4;
     if (!early) {
@@ -321,7 +327,7 @@ __device__ __forceinline__ void widen8(const SvlmCacheDev& cd, const SvlmStore8&
     }
     if (!here) return;
     const int unit = HALF_KEYS ? ld_l2(st.most + layer * cd.kv_heads + h) - MOST8_BIAS : 0;
-    if (HALF_KEYS && blockIdx.x == 0 && threadIdx.x == 0) reinterpret_cast<int*>(static_cast<unsigned char*>(cd.tmaps) + 512)[h] = unit;
+    if (HALF_KEYS && blockIdx.x == 0 && threadIdx.x == 0) heads_of(cd)[h].unit = unit;
     const size_t row0 = ((size_t)layer * cd.kv_heads + h) * cd.n_slots + (size_t)tile.x * SVLM_PAGE + off;
     uint2 raw[TOKENS][4];                                    // low and high halves of the key, of the value
     unsigned exps[TOKENS];
@@ -333,6 +339,28 @@ __device__ __forceinline__ void widen8(const SvlmCacheDev& cd, const SvlmStore8&
         raw[i][0] = two(k); raw[i][1] = two(k + HALF);
         raw[i][2] = two(v); raw[i][3] = two(v + HALF);
         exps[i] = live[i] ? ld_l2(st.exps + (row0 + 32 * i) / SVLM_BLOCK8) : 0;
+    }
+    if (HALF_KEYS) {                                         // values that are not finite: see svlm_store8.h
+        unsigned any = 0;
+#pragma unroll
+        for (int i = 0; i < TOKENS; ++i)
+#pragma unroll
+            for (int q = 2; q < 4; ++q) any |= nan_bytes(raw[i][q].x) | nan_bytes(raw[i][q].y);
+        if (__builtin_expect(any != 0, 0)) {
+            const long long first = ld_l2(&cd.ctrl->n_total) - n_q;
+#pragma unroll
+            for (int i = 0; i < TOKENS; ++i)
+                if (live[i] && ld_l2(cd.slot_gid + tile.x * SVLM_PAGE + off + 32 * i) > first)
+#pragma unroll
+                    for (int q = 2; q < 4; ++q)
+#pragma unroll
+                        for (int k = 0; k < 2; ++k) {
+                            unsigned& w = k ? raw[i][q].y : raw[i][q].x;
+                            const unsigned nan = nan_bytes(w);
+                            w &= ~(nan * 0xffu);
+                            if (nan) heads_of(cd)[h].late = 1;
+                        }
+        }
     }
 #pragma unroll
     for (int i = 0; i < TOKENS; ++i) {
@@ -369,15 +397,15 @@ __device__ __forceinline__ void widen8(const SvlmCacheDev& cd, const SvlmStore8&
 }
 
 template <int D, bool HALF_KEYS>
-__global__ void __launch_bounds__(2 * D) widen8_kernel(SvlmCacheDev cd, SvlmStore8 st, int layer, int early) {
-    widen8<D, HALF_KEYS>(cd, st, layer, early);
+__global__ void __launch_bounds__(2 * D) widen8_kernel(SvlmCacheDev cd, SvlmStore8 st, int layer, int n_q, int early) {
+    widen8<D, HALF_KEYS>(cd, st, layer, n_q, early);
 }
 // blockIdx.z: the cache (sixteen streams, 32/8 heads of 128 over 2,900 keys: 74 tokens each, append and attention 322 us a layer, 370 with a launch for each).
 template <int D, bool HALF_KEYS>
 __global__ void __launch_bounds__(2 * D) widen8_batch_kernel(SvlmCacheList list, SvlmStore8List stores, int layer, int early) {
     __shared__ SvlmCacheDev cd;
     svlm_load_desc(&cd, list.cd[blockIdx.z]);
-    widen8<D, HALF_KEYS>(cd, stores.at[blockIdx.z], layer, early);
+    widen8<D, HALF_KEYS>(cd, stores.at[blockIdx.z], layer, stores.n_q[blockIdx.z], early);
 }
 
 }  // namespace
@@ -402,9 +430,9 @@ cudaError_t svlm_launch_shift8(const SvlmCacheList& list, const SvlmStore8List& 
     return svlm_launch_chained(geom.head_dim == 128 ? shift8_kernel<128> : shift8_kernel<64>, dim3(geom.n_pages + geom.layers * geom.kv_heads, list.n), dim3(256), 0, 1, st, list, stores);
 }
 
-cudaError_t svlm_launch_widen8(const SvlmCacheDev& cd, const SvlmStore8& st8, int layer, bool half, bool early, cudaStream_t st) {
+cudaError_t svlm_launch_widen8(const SvlmCacheDev& cd, const SvlmStore8& st8, int layer, int n_q, bool half, bool early, cudaStream_t st) {
     const auto kernel = cd.head_dim == 128 ? (half ? widen8_kernel<128, true> : widen8_kernel<128, false>) : (half ? widen8_kernel<64, true> : widen8_kernel<64, false>);
-    return svlm_launch_chained(kernel, dim3(cd.n_pages, cd.kv_heads), dim3(2 * cd.head_dim), 0, 1, st, cd, st8, layer, (int)early);
+    return svlm_launch_chained(kernel, dim3(cd.n_pages, cd.kv_heads), dim3(2 * cd.head_dim), 0, 1, st, cd, st8, layer, n_q, (int)early);
 }
 
 cudaError_t svlm_launch_widen8_batch(const SvlmCacheList& list, const SvlmStore8List& stores, const SvlmCacheDev& geom, int layer, bool half, bool early, cudaStream_t st) {

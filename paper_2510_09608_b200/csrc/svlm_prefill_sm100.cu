@@ -288,6 +288,7 @@ struct PfGroup {
     long long n_total, shift;
     int first[PF_LIST];      // smallest ordinals of the first pages of its list, relative to the first query token
     unsigned merge_later;    // blocks of columns of the first segment's unit that this CTA has to merge at the end
+    int late;                // HALF: the head has values that late_values must look for
 };
 
 struct PfShared {            // control part of shared memory, behind the tiles
@@ -404,6 +405,45 @@ __device__ __forceinline__ void softmax_page(int g, const PfTmem& t, unsigned mi
     bar_arrive(BAR_P2 + g, 160);
 }
 
+
+// HALF: a chunk's own values that are not finite lie as zeros in the widened layer (0 times NaN would reach the rows that do not see them).  A row's outputs in
+// the dims in which a token up to its own has one become NaN here, behind the segment's last product.  Seldom run, and so outside the caller's registers.
+template <int D>
+__device__ __noinline__ void late_values(const SvlmAttendView& vw, int n_tiles, long long gid_q0, const unsigned char* V8, int r, unsigned tO) {
+#pragma unroll 1
+    for (int q = 0; q < D; q += 16) {
+        unsigned mine = 0;                                   // this row's of the 16 dims
+#pragma unroll 1
+        for (int t = 0; t < n_tiles; ++t) {
+            const PfEntry e = pf_load_entry(vw, t, gid_q0);
+            if (e.last <= 0) continue;
+            const int first = (int)(e.info & 0x3FFF) * SVLM_PAGE, lo = (e.info >> 14) & 127, hi = ((e.info >> 21) & 127) + 1;
+#pragma unroll 1
+            for (int o = lo; o < hi; ++o) {
+                const long long rel = ld_l2(vw.slot_gid + first + o) - gid_q0;
+                if (rel <= 0) continue;                      // (all rows see it: its values are in the layer)
+                const uint4 v = ld_l2(reinterpret_cast<const uint4*>(V8 + (size_t)(first + o) * D + q));
+                const unsigned w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const unsigned nan = (((w[k] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) >> 7;
+                    if (rel <= r) mine |= ((nan & 1) | (nan >> 7 & 2) | (nan >> 14 & 4) | (nan >> 21 & 8)) << (4 * k);
+                }
+            }
+        }
+        if (!__any_sync(0xffffffffu, mine != 0)) continue;
+#pragma unroll 1
+        for (int k = 0; k < 16; k += 8) {
+            float o[8];
+            tmem_ld8(tO + q + k, o);
+            tmem_wait_ld<8>(o);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) o[i] = (mine >> (k + i)) & 1 ? __int_as_float(0x7fffffff) : o[i];
+            tmem_st8(tO + q + k, o);
+        }
+    }
+    tmem_wait_st();
+}
 
 // A warp's walk over the pages of a segment, 32 entries of the cache's page list at a time, one per lane.
 struct PfPages {
@@ -1191,7 +1231,11 @@ prefill_kernel(const __grid_constant__ SvlmAttendBatch b, const __grid_constant_
             PfPages pages;
             pages.begin(sh);
             // the power of two of the head's keys stands behind the cache's descriptors
-            if (HALF) unit += ld_l2(reinterpret_cast<const int*>(reinterpret_cast<const unsigned char*>(w.vw->tmaps) + 512) + gr.rows.hk);
+            if (HALF) {
+                const long long head = ld_l2(reinterpret_cast<const long long*>(reinterpret_cast<const unsigned char*>(w.vw->tmaps) + 512) + gr.rows.hk);      // SvlmHead8
+                unit += (int)head;
+                if (m == 0) gr.late = (int)(head >> 32);
+            }
             // (Not below 2^-120, so that c_row is a normal number: a row of zeros has the least unit there is, and a hidden score, -inf, times 0 would be NaN.)
             const float c_row = pf_scale<D> * __int_as_float((127 + max(-120, min(120, unit))) << 23);
             for (int j = 0; j < n_proc; ++j) {
@@ -1229,6 +1273,8 @@ prefill_kernel(const __grid_constant__ SvlmAttendBatch b, const __grid_constant_
             tc_fence_after();
             ok = !*abort_flag;                // (of a wait that has run out nothing is known here: the barriers go on in their order)
             const bool have_o = ok && n_proc > 0;
+            if (HALF && have_o && __builtin_expect(gr.late, 0))      // (written behind the barriers of the pages)
+                late_values<D>(*w.vw, w.n_tiles, w.gid_q0, w.vw->tagged + (size_t)gr.rows.hk * b.n_slots * D, r, tm.O);
             if (gr.seg.e - gr.seg.a == PF_FRAC) {                      // all of the unit's pages
                 const float inv = l > 0.f ? 1.f / l : 0.f;
                 const int mg = mt + m;

@@ -627,7 +627,7 @@ rows8_kernel(SvlmAttend8 a, int layer0, int n_layers, const uint16_t* Q, const i
                 for (int k = 0; k < 4; ++k)
 #pragma unroll
                     for (int w = 0; w < C::VW; ++w) {
-                        const unsigned nan = (((v[k][w] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) >> 7;
+                        const unsigned nan = nan_bytes(v[k][w]);
                         any |= nan != 0;
                         v[k][w] &= ~(nan * 0xffu);
                     }

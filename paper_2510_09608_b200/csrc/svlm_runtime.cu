@@ -124,6 +124,9 @@ void fill_view(const svlm_cache* c, SvlmAttendView& v) {
     v.tagged = c->decode_tagged;
 }
 
+// A layer's values of an 8-bit cache, as the chunk kernel looks them up (SvlmAttendView::tagged).
+unsigned char* values8(const svlm_cache* c, int layer) { return c->store8.V + (size_t)layer * c->dev.kv_heads * c->dev.n_slots * c->dev.head_dim; }
+
 // Rotation table: (cos, sin)(k * 256^level * theta_i) in fp32 from fp64 (see svlm_rope.cuh).  k = 16 a + b: the 16
 // multiples of either kind are evaluated, their 256 sums follow by the angle-addition identity in fp64 (error ~3e-16).
 int upload_rope_table(svlm_cache* c) {
@@ -309,10 +312,10 @@ int shift8(svlm_cache* const* caches, int n_caches) {
     return SVLM_OK;
 }
 
-// 8-bit caches: one layer of each in 16 bits in front of the attention over it.
-int widen(svlm_cache* const* caches, int n_caches, int layer, bool half) {
+// 8-bit caches: one layer of each in 16 bits in front of the attention of n_q rows (each: of so many of each cache) over it.
+int widen(svlm_cache* const* caches, int n_caches, int layer, int n_q, const int32_t* each, bool half) {
     if (n_caches == 1) {
-        SVLM_CUDA(svlm_launch_widen8(caches[0]->dev, caches[0]->store8, layer, half, caches[0]->meta_settled, caches[0]->stream));
+        SVLM_CUDA(svlm_launch_widen8(caches[0]->dev, caches[0]->store8, layer, each ? each[0] : n_q, half, caches[0]->meta_settled, caches[0]->stream));
         return SVLM_OK;
     }
     bool settled = true;
@@ -320,6 +323,7 @@ int widen(svlm_cache* const* caches, int n_caches, int layer, bool half) {
     SvlmCacheList list;
     SvlmStore8List stores;
     list_stores(caches, n_caches, list, stores);
+    for (int i = 0; i < n_caches; ++i) stores.n_q[i] = each ? each[i] : n_q;
     SVLM_CUDA(svlm_launch_widen8_batch(list, stores, caches[0]->dev, layer, half, settled, caches[0]->stream));
     return SVLM_OK;
 }
@@ -432,7 +436,10 @@ int attend_common(svlm_cache* const* caches, int n_caches, int layer, const void
     SvlmAttendBatch b;
     b.n_caches = n_caches;
     fill_batch_geometry(c0, b);
-    for (int i = 0; i < n_caches; ++i) fill_view(caches[i], b.view[i]);
+    for (int i = 0; i < n_caches; ++i) {
+        fill_view(caches[i], b.view[i]);
+        if (c0->bits8) b.view[i].tagged = values8(caches[i], std::max(layer, 0));
+    }
     if (few8) {
         SvlmAttend8 a;
         fill_attend8(caches, n_caches, a);
@@ -449,7 +456,7 @@ int attend_common(svlm_cache* const* caches, int n_caches, int layer, const void
     const int n_layers = layer < 0 ? c0->dev.layers : 1;
     int early = 0;
     if (c0->bits8) {
-        const int rc = widen(caches, n_caches, std::max(layer, 0), chunk);
+        const int rc = widen(caches, n_caches, std::max(layer, 0), n_q, nullptr, chunk);
         if (rc != SVLM_OK) return rc;
     }
     if (n_q == 1 && layer >= 0 && !c0->bits8) {
@@ -590,7 +597,7 @@ int create(svlm_cache** out, int layers, int kv_heads, int head_dim, int n_sink,
         mem.add(&c->rows8_scratch, svlm_rows8_scratch_bytes(head_dim));
         mem.add(&c->rows8_tagged, svlm_rows8_tagged_bytes(kv_heads, head_dim));
     }
-    mem.add(reinterpret_cast<unsigned char**>(&d.tmaps), 512 + (bits8 ? (size_t)kv_heads * sizeof(int) : 0));
+    mem.add(reinterpret_cast<unsigned char**>(&d.tmaps), 512 + (bits8 ? (size_t)kv_heads * sizeof(SvlmHead8) : 0));
     mem.add(&d.rope_tab, (size_t)3 * 256 * (head_dim / 2) * 2, false);
     mem.add(&c->dev_copy, 1);
     const size_t slot_bytes = svlm_prefill_slot_bytes(d.n_pages, head_dim);
@@ -908,7 +915,8 @@ int svlm_attend_batched_varlen(svlm_cache* const* caches, int n_caches, int laye
         return SVLM_OK;
     }
     if (c0->bits8) {
-        rc = widen(caches, n_caches, layer, true);
+        rc = widen(caches, n_caches, layer, n_max, n_q, true);
+        for (int i = 0; i < n_caches; ++i) b.view[i].tagged = values8(caches[i], layer);
         if (rc != SVLM_OK) return rc;
         layer = 0;
     }
@@ -1163,7 +1171,7 @@ int svlm_cache_read_kv(svlm_cache* c, int layer, void* K_host, void* V_host) {
     const size_t per_layer = (size_t)d.kv_heads * d.n_slots * d.head_dim;
     std::vector<uint16_t> slab(per_layer);
     if (c->bits8) {
-        rc = widen(&c, 1, layer, false);
+        rc = widen(&c, 1, layer, 0, nullptr, false);
         if (rc != SVLM_OK) return rc;
         SVLM_CUDA(cudaStreamSynchronize(c->stream));
         layer = 0;

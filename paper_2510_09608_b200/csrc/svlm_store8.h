@@ -33,7 +33,10 @@ struct SvlmStore8 {
 };
 constexpr int MOST8_BIAS = 128;
 constexpr int MIXED8 = -1;   // (S >= s: a shift only grows along the stream)
-struct SvlmStore8List { SvlmStore8 at[SVLM_MAX_BATCH]; };
+struct SvlmStore8List {
+    SvlmStore8 at[SVLM_MAX_BATCH];
+    int n_q[SVLM_MAX_BATCH]; // query rows of the attention over what is widened
+};
 
 // Behind an eviction's metadata: apart and turn of every active page's blocks.
 cudaError_t svlm_launch_shift8(const SvlmCacheList& list, const SvlmStore8List& stores, const SvlmCacheDev& geom, cudaStream_t st);
@@ -45,8 +48,10 @@ cudaError_t svlm_launch_kv_write8(const SvlmCacheDev& cd, const SvlmStore8& st8,
                                   bool early, cudaStream_t st);
 // One layer's stored keys, rotated at their contiguous positions, and values in 16 bits in cd.K and cd.V ([kv_heads][n_slots][head_dim]):
 // all slots of the active pages, those without a token as zeros.  Values are bf16 (exact).  Keys are bf16, or (half) f16 in units of a power
-// of two of their KV head, whose exponent goes 512 bytes behind cd.tmaps.
-cudaError_t svlm_launch_widen8(const SvlmCacheDev& cd, const SvlmStore8& st8, int layer, bool half, bool early, cudaStream_t st);
+// of two of their KV head.  Its exponent goes into SvlmHead8; and there, values that are not finite of tokens that come behind the first of the latest n_q are
+// zeros, since the rows before them must not have them, and late says so: the chunk kernel puts them into the others (from the bytes).
+struct SvlmHead8 { int unit, late; };    // per KV head, 512 bytes behind cd.tmaps; late stays until an eviction
+cudaError_t svlm_launch_widen8(const SvlmCacheDev& cd, const SvlmStore8& st8, int layer, int n_q, bool half, bool early, cudaStream_t st);
 cudaError_t svlm_launch_widen8_batch(const SvlmCacheList& list, const SvlmStore8List& stores, const SvlmCacheDev& geom, int layer, bool half, bool early,
                                      cudaStream_t st);
 

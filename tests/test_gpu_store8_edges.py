@@ -342,3 +342,53 @@ def test_a_giant_that_stays_when_another_has_left_its_block(d, by):
         Q[..., d // 2 - 1], Q[..., d // 2 - 2] = sign, 2 * sign
         got = dev_to_f64(p.cache.attend(0, to_dev(Q), torch.from_numpy(np.ascontiguousarray(pos)).cuda()))
         close(got, p.ref.attend(0, Q, pos))
+
+
+@pytest.mark.parametrize("bad", [np.nan, -np.inf])
+@pytest.mark.parametrize("hq,hk,d,before,n", [(8, 2, 128, 150, 170), (8, 2, 64, 1500, 200), (28, 4, 128, 1700, 140)])
+def test_a_value_that_is_not_finite_stays_out_of_the_rows_before_it_in_a_long_chunk(hq, hk, d, before, n, bad):
+    """Values of a chunk that goes over a widened layer which are not finite, in several of its pages and in an earlier token: the rows that see them have
+    NaN in those dims only, the rows of tokens before them are as ever.  One cache and two at once; the next layer and the next chunk have none of it."""
+    G = hq // hk
+    ps = [Pair(1000 + i, layers=2, hq=hq, hk=hk, d=d, sink=4, vw=before + 100, tw=100, capacity=before + 2 * n + 300) for i in range(2)]
+    spots = [((3, 0, 7), (n // 2, 0, 7), (n // 2, 0, d // 2), (n // 2 + 1, hk - 1, d - 1), (n - 1, 0, 0)), ((0, 0, 1), (n - 2, hk - 1, 3))]
+    news, Qs = [], []
+    for p, where in zip(ps, spots):
+        p.append(p.rng.integers(0, 2, before))
+        p.evict()
+        V = p.normal(2, n, hk, d)
+        clean = V.copy()
+        for tok, head, dim in where:
+            V[0, tok, head, dim], clean[0, tok, head, dim] = bad, 0
+        types = np.ones(n, np.uint8)
+        types[-20:] = 0
+        p.ref.append(types, pos := p.place(types), K := p.normal(2, n, hk, d), clean)
+        p.pos = pos
+        p.cache.append(-1, to_dev(K), to_dev(V), torch.from_numpy(types).cuda(), torch.from_numpy(pos).cuda())
+        Qs.append(bf16(p.rng.standard_normal((2, n, hq, d))))
+        lost = np.zeros((n, hq, d), bool)
+        for tok, head, dim in where:
+            lost[tok:, head * G:(head + 1) * G, dim] = True
+        news.append((pos, lost))
+
+    def see(got, i, layer):
+        want, lost = ps[i].ref.attend(layer, Qs[i][layer], news[i][0]), news[i][1] if layer == 0 else np.zeros_like(news[i][1])
+        assert ps[i].cache.status() == binding.OK and np.array_equal(np.isnan(got), lost)
+        close(got[~lost], want[~lost])
+    for layer in (0, 1, 0):
+        for i, p in enumerate(ps):
+            see(dev_to_f64(p.cache.attend(layer, to_dev(Qs[i][layer]), torch.from_numpy(news[i][0]).cuda())), i, layer)
+        both = binding.attend_batched_varlen([p.cache for p in ps], layer, to_dev(np.concatenate([q[layer] for q in Qs])),
+                                             torch.from_numpy(np.concatenate([x[0] for x in news])).cuda(), [n, n])
+        for i in range(2):
+            see(dev_to_f64(both[i * n:(i + 1) * n]), i, layer)
+    for p in ps:                                             # the chunk's tokens are earlier ones now, and then gone
+        for _ in range(3):
+            p.append([1] * (before + 100) if before < 1000 else [1] * n)
+            p.evict()
+    if before < 1000:
+        for p in ps:
+            p.append([0] * 110 + [1] * n)
+            p.evict()
+            p.append([1] * n)
+            p.attend(n)
