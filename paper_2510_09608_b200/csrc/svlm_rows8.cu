@@ -30,10 +30,13 @@
 // behind the wait there are the query, scores and outputs of units that are there already, and the meeting of the splits, as tagged words
 // that the first thread blocks of a KV head poll for, each combining a share (see combine_tagged).
 //
-// What bounds it: the chain of a unit's steps (conversions, MMAs, maxima, exponentials), some 520 instructions of which a warp issues one in six cycles; of
-// DRAM's rate a launch reaches 0.4 (sixteen streams), with fewer keys the chain's length is all that counts.  Measured, 28/4 heads of 128, us a layer-step in a
-// graph: 7.2 over 9216 keys with 28 layers in a row (1.4 at the copy rate), 6.2 over 512, 18.2 over 44512; sixteen streams of 9216 keys 45 (23); 32/8 heads over
-// 44512 keys 32 (14); nine tokens' chunk over 9216 keys 30.  A stream that has just moved on, most of whose units have shifts of their own, 8.5.
+// What bounds it: the latency of a unit's steps one after another (conversions, MMAs, maxima, exponentials: some 520 instructions, of which a warp issues
+// one in six cycles), with sixteen warps an SM at most to hide it.  No unit of the SM is full: sixteen streams have the issue slots 33 % busy, the
+// integer pipe 45 %, the tensor pipe 12 % and DRAM 35 %, and 256 blocks on 296 places, so that some SMs have one and wait for those with two.  With fewer keys the chain's
+// length is all that counts.  Measured, 28/4 heads of 128, us a layer-step in a
+// graph: 7.2 over 9216 keys with 28 layers in a row (1.4 at the copy rate; the 16-bit cache's kernel, which has nothing to convert, 6.0), 6.2 over 512, 18.2 over
+// 44512; sixteen streams of 9216 keys 45 (23); 32/8 heads over
+// 44512 keys 32 (14); nine tokens' chunk over 9216 keys 27.  A stream that has just moved on, most of whose units have shifts of their own, 8.5.
 // Tried: keys made into fragments before the wait (10 us), runs of 4 units dealt out in turn (sixteen streams 52, nine rows over 44512 keys 84 instead of 118).
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -144,8 +147,9 @@ __device__ __forceinline__ int chunk_at(int row, int chunk) { return row * D + (
 // One query token's outputs from the splits' tagged records: the first `shares` splits of a KV head take groups of eight output elements each.
 // Eight lanes cover eight groups, which lie side by side in a record; the lane groups of all warps take 32 records at a time, two rounds in
 // flight.  A word that does not carry the tag yet is read again, wait_limit times at most; then the status word says so and what there is
-// is written.  All thread blocks of the launch are resident together (one wave of them, and a dependent launch enters only when
-// all of them have passed their trigger), so the wait is for stragglers.
+// is written.  All thread blocks of the launch have places together (one wave of them, and a dependent launch enters only when
+// all of them have passed their trigger), so the wait is for stragglers; beside other streams' launches it is for those to end, too: only these first
+// splits of a launch ever wait, and the others leave their places by themselves.
 template <int D>
 __device__ __forceinline__ void combine_tagged(int share, int shares, int splits, const unsigned char* parts, unsigned tag, float* buf, int G,
                                                uint16_t* out_row0, unsigned wait_limit, int* status) {

@@ -9,9 +9,10 @@
 // (programmatic dependent launch) a warp asks for its first four blocks; behind the wait come the activations.  The warps' sums meet in
 // shared memory and are added in their order: the same bits every time.
 //
-// Bound by the turning of nibbles beside the loads: some 72 operations of the integer pipe for 1 KB of weights, of 8192 -> 24576 17 us, and 19 us the loads alone.
-// Measured (inputs -> outputs, group 128 unless said, back to back in a graph, weights out of DRAM; in brackets the bytes at the copy rate): one token
-// 3584 -> 4608 3.7 us (1.3), group 32 6.7; two 8192 -> 24576 28 us, 3.7 TB/s (16); sixteen 3584 -> 3584, group 64, 5.1 us (1.1); thirty-two 3584 -> 4608 11.2 us
+// Of 8192 -> 24576 the turning of nibbles is 17 us of the integer pipe (some 72 operations for 1 KB of weights) and the loads alone take 19; together they take 27, with
+// neither full (the pipe 52 % busy, DRAM 40 %): a warp's loads and its products take turns, and sixteen warps an SM do not hide that.
+// Measured (inputs -> outputs, group 128 unless said, back to back in a graph; in brackets the bytes at the copy rate; a matrix of up to 126 MB may be in L2 in
+// part when it is read again): one token 3584 -> 4608 3.7 us (1.3), group 32 6.7; two 8192 -> 24576 27 us, 3.9 TB/s (16); sixteen 3584 -> 3584, group 64, 5.1 us (1.1); thirty-two 3584 -> 4608 11.2 us
 // (1.4).  From sixteen tokens on each 16 features read all activations again, and that is what bounds it.  Tried: a cluster of eight blocks for 128
 // features, each with an eighth of K and its share of the activations in shared memory: 9.0 us, 52 us, 8.7 us, 16.7 us.
 #include <cuda_bf16.h>
