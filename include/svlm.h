@@ -69,7 +69,7 @@ int svlm_cache_create(svlm_cache** out, int layers, int kv_heads, int head_dim, 
 /*
  * A cache that holds its keys and values in 8 bits: half the memory, half the bytes that a decode step reads, and an eviction that moves no keys.
  * Streams that generate in lock step gain time by it (28/4 heads of 128 over 9216 keys, sixteen streams: 45 us a step, a 16-bit cache 55).  One stream by
- * itself does not, since its steps are bound by latency and 8 bits have to be converted: a token's layer 7.2 us and 6.0, a chunk of 524
+ * itself does not, since its steps are bound by latency and 8 bits have to be converted: a token's layer 7.1 us and 6.0, a chunk of 524
  * tokens 91 us a layer and 79, four tokens of the smallest stream 44 and 34.
  * Every other entry point takes such a cache as it takes one of svlm_cache_create (the same inputs and outputs in bf16, the same
  * policy and positions), except

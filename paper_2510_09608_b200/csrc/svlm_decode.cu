@@ -1364,11 +1364,7 @@ decode_layer_kernel(SvlmAttendBatch b, int layer, const uint16_t* Q, const int* 
 #else
     auto stamp7 = [](int) {};
 #endif
-    if (threadIdx.x == 0) {
-        const unsigned tag = (unsigned)(asked >> 32) + 1;
-        sh.tag = (int)tag;
-        if ((unsigned)asked == (unsigned)splits - 1) __stcg(epoch, (unsigned long long)tag << 32);   // nobody else asks before this launch has ended
-    }
+    if (threadIdx.x == 0) sh.tag = (int)(asked >> 32) + 1;
     cta_merge_and_record<D, true>(o, m, l, reinterpret_cast<float*>(ring), part, stamp7, &sh.tag);
     if constexpr (Append::on) {
         if (warp == DEC_CWARPS - 1) write_token_down(app, ci, sh.one, new_slot, before, gridDim.x * gridDim.y);
@@ -1377,6 +1373,8 @@ decode_layer_kernel(SvlmAttendBatch b, int layer, const uint16_t* Q, const int* 
     // ---- the first splits of this KV head combine all the splits' records -----------------------------
     __syncthreads();                                  // the merge slabs in `ring` are read
     if (threadIdx.x == 0) STAMP(8);                   // the CTA's record is on its way
+    // the last to ask moves the epoch on; nobody else asks before this launch has ended
+    if (threadIdx.x == 0 && (unsigned)asked == (unsigned)splits - 1) __stcg(epoch, ((asked >> 32) + 1) << 32);
     const int shares = combine_shares(G * (D / 8), splits);
     if (split >= shares) {
         if (threadIdx.x == 0) STAMP(13);

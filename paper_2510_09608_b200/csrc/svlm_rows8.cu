@@ -34,7 +34,7 @@
 // one in six cycles), with sixteen warps an SM at most to hide it.  No unit of the SM is full: sixteen streams have the issue slots 33 % busy, the
 // integer pipe 45 %, the tensor pipe 12 % and DRAM 35 %, and 256 blocks on 296 places, so that some SMs have one and wait for those with two.  With fewer keys the chain's
 // length is all that counts.  Measured, 28/4 heads of 128, us a layer-step in a
-// graph: 7.2 over 9216 keys with 28 layers in a row (1.4 at the copy rate; the 16-bit cache's kernel, which has nothing to convert, 6.0), 6.2 over 512, 18.2 over
+// graph: 7.1 over 9216 keys with 28 layers in a row (1.4 at the copy rate; the 16-bit cache's kernel, which has nothing to convert, 6.0), 6.2 over 512, 18.2 over
 // 44512; sixteen streams of 9216 keys 45 (23); 32/8 heads over
 // 44512 keys 32 (14); nine tokens' chunk over 9216 keys 27.  A stream that has just moved on, most of whose units have shifts of their own, 8.5.
 // Tried: keys made into fragments before the wait (10 us), runs of 4 units dealt out in turn (sixteen streams 52, nine rows over 44512 keys 84 instead of 118).
@@ -96,10 +96,9 @@ __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_gr
 // the next launch took for its own.)
 // (The answer is looked at when it is wanted, behind the outputs: looked at as soon as it has been asked for, it held up thread 0's queries by 0.13 us.)
 __device__ __forceinline__ unsigned long long ask_tag(unsigned long long* epoch) { return atomicAdd(epoch, 1ull); }      // { epoch, blocks that have asked }
-__device__ __forceinline__ unsigned tag_of(unsigned long long asked, unsigned long long* epoch, int splits) {
-    const unsigned tag = (unsigned)(asked >> 32) + 1;
-    if ((unsigned)asked == (unsigned)splits - 1) __stcg(epoch, (unsigned long long)tag << 32);      // nobody else asks before this launch has ended
-    return tag;
+__device__ __forceinline__ unsigned tag_of(unsigned long long asked) { return (unsigned)(asked >> 32) + 1; }
+__device__ __forceinline__ void move_on(unsigned long long asked, unsigned long long* epoch, int splits) {      // nobody else asks before this launch has ended
+    if ((unsigned)asked == (unsigned)splits - 1) __stcg(epoch, (unsigned long long)tag_of(asked) << 32);
 }
 __device__ __forceinline__ void st_tagged2(void* p, unsigned a, unsigned b, unsigned tag) {
     const unsigned long long hi = (unsigned long long)tag << 32;
@@ -950,7 +949,7 @@ rows8_kernel(SvlmAttend8 a, int layer0, int n_layers, const uint16_t* Q, const i
             }
         }
     }
-    if (LAYER && threadIdx.x == 0) sh.tag = (int)tag_of(asked, epoch, splits);
+    if (LAYER && threadIdx.x == 0) sh.tag = (int)tag_of(asked);
     __syncthreads();
     const int n_cols = min(C::COLS, m_total - m0);
     // (token r, head h) of column m lies at row r * q_heads + h = r * (q_heads - G) + m
@@ -994,6 +993,7 @@ rows8_kernel(SvlmAttend8 a, int layer0, int n_layers, const uint16_t* Q, const i
     if (splits == 1) return;
     __syncthreads();                               // the merge buffer is read, the records are on their way
     if (LAYER) {
+        if (threadIdx.x == 0) move_on(asked, epoch, splits);
         const int groups = G * CH, shares = min((groups + R8_GROUPS - 1) / R8_GROUPS, splits);
         if (split < shares)
             combine_tagged<D>(split, shares, splits, parts, (unsigned)sh.tag, merge, G, out + (q_row0 * q_heads + hk * G) * D, sh.wait_limit,
